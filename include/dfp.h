@@ -429,6 +429,130 @@ dfp_status dfp_sgd_quantize(int64_t n, float lr, float mu, float wd, int32_t bit
                             uint64_t seed, float* w, float* v, const float* dw, int16_t* wq, dfp_scale* sw,
                             void* stream);
 
+/* ---------------------------------------------------- INT8 linear layers --
+ * The products of a language model's linear layers in 8-bit integers: one FP32
+ * scale per token (row of the activations) and per output channel (row of the
+ * weights).  Real scales, not powers of two: at 8 bits the factor of up to two
+ * that a power of two leaves unused is a bit of eight.
+ *
+ *   quantise   a_r = max over c of |x[r][c]|, s_r = fl32(a_r / 127),
+ *              q[r][c] = round(x[r][c] / s_r) of the exact quotient, in
+ *              [-127, 127].  NEAREST: ties to even.  STOCHASTIC: with
+ *              qn the nearest integer, e = x - qn s (exact) and
+ *              R = floor(fl32(e / s) 2^32): q = qn + floor(R / 2^32) +
+ *              (U < R mod 2^32), U the Philox word of the element's flat index
+ *              r * cols + c and the role, as in dfp_quantize.  A row of zeros
+ *              (or one so small that s_r rounds to 0): q = 0, s_r = 0.  A row
+ *              with NaN or Inf: q = 0, s_r = NaN, so what is computed from that
+ *              row is NaN and the other rows are unaffected.
+ *   product    y[m][n] = fl(S sa[m] sb[n] + bias[n]), S the exact INT32 sum
+ *              over k of a[m][k] b[n][k]; converted to FP32, scaled and added
+ *              in FP32 in this order, rounded once to the output type.
+ *   forward    xq, sx = quantise(x); y = product(xq, wq): y = x W^T + bias.
+ *   backward   dx = dy W: the scale of the summed index goes with the gradient,
+ *     -data    g = fl32(dy[m][n] sw[n]); gq, sg = quantise(g) per token;
+ *              dx[m][k] = fl(S sg[m]), S = sum over n of gq[m][n] wq[n][k].
+ *   backward   dW = dy^T x: g = fl32(dy[m][n] sx[m]); gq, sg = quantise of g per
+ *     -weights output channel n over the tokens; dw[n][k] = fl32(S sg[n]),
+ *              S = sum over m of gq[m][n] xq[m][k]; db[n] = sum over m of dy.
+ *
+ * Layouts.  x, y, dy, dx: row-major, densely packed, of the descriptor's type.
+ * INT8 operands: [rows][ld], ld = dfp_i8_ld(cols) = cols rounded up to 128, the
+ * padding bytes ZERO (dfp_quantize_i8 writes them).  Transposed operands (wqt,
+ * xqt) are the same integers as [cols][dfp_i8_ld(rows)].  Tensors and INT8
+ * operands 16-byte aligned, scales and biases 4-byte.
+ * Sizes: every dimension >= 1; k (and n for backward-data, m for
+ * backward-weights: the summed one) at most DFP_I8_MAX_SUM, so that no INT32
+ * sum overflows whatever the integers are. */
+typedef enum dfp_type { DFP_F32 = 0, DFP_BF16 = 1, DFP_F16 = 2 } dfp_type;
+#define DFP_I8_MAX_SUM 131071
+
+/* y [m][n] = x [m][k] W^T, W [n][k]. */
+typedef struct dfp_linear_desc {
+  int32_t m, n, k;  /* tokens, output features, input features                  */
+  int32_t type;     /* dfp_type of x, y, dy, dx (dw, db, bias and scales: FP32) */
+  int32_t rounding; /* NEAREST or STOCHASTIC, of x (forward) and g (backward)   */
+  uint64_t seed;    /* Philox key; the streams are those of roles X and DY      */
+} dfp_linear_desc;
+
+/* Bytes of a row of cols integers: cols rounded up to 128; 0 if cols < 1. */
+int64_t dfp_i8_ld(int64_t cols);
+
+/* Rows of src [rows][cols] (a dfp_type) to INT8.  q: [rows][dfp_i8_ld(cols)];
+ * scale: FP32 [rows]; qt (nullable): the transpose, [cols][dfp_i8_ld(rows)].
+ * rows and cols at most 2^31 - 256 each, rows * ld at most 2^40. */
+dfp_status dfp_quantize_i8(int64_t rows, int64_t cols, int32_t type, int32_t rounding, uint64_t seed, int32_t role,
+                           const void* src, int8_t* q, float* scale, int8_t* qt, void* stream);
+
+/* The product alone: a [m][ld(k)], sa FP32 [m], b [n][ld(k)], sb FP32 [n], bias
+ * (nullable) FP32 [n], out [m][n] of the descriptor's type. */
+dfp_status dfp_gemm_i8(const dfp_linear_desc* d, const int8_t* a, const float* sa, const int8_t* b, const float* sb,
+                       const float* bias, void* out, void* workspace, size_t ws_bytes, void* stream);
+
+/* Forward.  x [m][k]; wq [n][ld(k)], sw [n]; bias (nullable) [n]; y [m][n].
+ * For the backward calls, each nullable: sx FP32 [m], the scales of the tokens,
+ * and xqt [k][ld(m)], their integers transposed; xq [m][ld(k)], the integers. */
+dfp_status dfp_linear_i8_fwd(const dfp_linear_desc* d, const void* x, const int8_t* wq, const float* sw,
+                             const float* bias, void* y, int8_t* xq, float* sx, int8_t* xqt, void* workspace,
+                             size_t ws_bytes, void* stream);
+/* Backward-data.  dy [m][n]; wqt [k][ld(n)], sw [n]; dx [m][k]. */
+dfp_status dfp_linear_i8_bwd_data(const dfp_linear_desc* d, const void* dy, const int8_t* wqt, const float* sw,
+                                  void* dx, void* workspace, size_t ws_bytes, void* stream);
+/* Backward-weights.  dy [m][n]; xqt [k][ld(m)], sx [m]; dw FP32 [n][k]; db
+ * (nullable) FP32 [n]. */
+dfp_status dfp_linear_i8_bwd_weights(const dfp_linear_desc* d, const void* dy, const int8_t* xqt, const float* sx,
+                                     float* dw, float* db, void* workspace, size_t ws_bytes, void* stream);
+/* Workspace bytes that serve every one of these calls on d; 0 for an invalid
+ * descriptor (k, n and m need not all be within DFP_I8_MAX_SUM for it).
+ * 256-byte aligned.  Nothing in it needs to start at zero or is read by a later
+ * call; calls in flight at once need one each. */
+size_t dfp_linear_i8_workspace_bytes(const dfp_linear_desc* d);
+
+/* -------------------------------------------------- orthogonalised updates --
+ * The update of a weight matrix made (nearly) orthogonal by Newton-Schulz
+ * products: for every matrix U [rows][cols] of a batch
+ *   X = U / (|U|_F + eps);  steps times, with coefficients (a, b, c) of the step:
+ *   A = X X^T, B = b A + c A A, X = a X + B X     (X^T X where rows > cols),
+ * which applies x -> a x + b x^3 + c x^5 to the singular values.
+ * Precision: X is held in FP32.  BF16 results: the products take X, A and B
+ * rounded to f16 (X in units of 2^-12, A of 2^-10, B's diagonal apart in FP32) and
+ * sum in FP32: 0.4e-3 to 0.9e-3 of the result's norm for matrices of some size, at
+ * most 2^-9, half of BF16's half step, for a few elements too.  FP32 and F16 results and dfp_muon_quantize: every operand is the
+ * sum of two f16 numbers and every product the sum of three: 1e-6 to 2e-5, what
+ * FP32 products give.  The units suit singular values up to 4 at every step (a, b,
+ * c that map [0, 1] further out overflow f16 and give Inf or NaN) and norms not
+ * below eps by more than a factor of 2^10 (smaller ones lose bits).  A zero
+ * matrix gives zeros; one with NaN or Inf gives NaN throughout. */
+#define DFP_ORTHO_MAX_STEPS 16
+typedef struct dfp_ortho_desc {
+  int32_t batch, rows, cols; /* >= 1; rows, cols <= 65536; batch <= 65535; batch
+                                times the padded matrix at most 2^40 elements  */
+  int32_t type;              /* dfp_type of x and out, or of dw                */
+  int32_t steps;             /* 1 .. DFP_ORTHO_MAX_STEPS                       */
+  float eps;                 /* finite, > 0                                    */
+  float coef[DFP_ORTHO_MAX_STEPS][3]; /* a, b, c of each step, finite, |.| <= 64 */
+} dfp_ortho_desc;
+
+/* out = the orthogonalised x; [batch][rows][cols] of the descriptor's type,
+ * densely packed, 16-byte aligned; out may be x. */
+dfp_status dfp_orthogonalize(const dfp_ortho_desc* d, const void* x, void* out, void* workspace, size_t ws_bytes,
+                             void* stream);
+
+/* One weight step by orthogonalised momentum, in place, on FP32 master weights
+ * w and momentum v [batch][rows][cols], dw the gradient (the descriptor's type):
+ *   v = fma(mu, v, dw);  u = nesterov ? fma(mu, v, dw) : v;
+ *   w = fma(-lr scale, O(u), (1 - lr wd) w)
+ * with lr scale and 1 - lr wd rounded to FP32 on the host, O as above; then, with
+ * wq, the rows of the new w (batch * rows of them) to INT8 as dfp_quantize_i8
+ * does (NEAREST): wq [batch*rows][ld(cols)], sw FP32 [batch*rows], wqt (nullable,
+ * batch = 1 only) [cols][ld(rows)].  wq and sw both or neither. */
+dfp_status dfp_muon_quantize(const dfp_ortho_desc* d, float lr, float mu, float wd, float scale, int32_t nesterov,
+                             float* w, float* v, const void* dw, int8_t* wq, float* sw, int8_t* wqt, void* workspace,
+                             size_t ws_bytes, void* stream);
+/* Workspace bytes of both calls; 0 for an invalid descriptor.  256-byte aligned;
+ * as for the INT8 calls. */
+size_t dfp_ortho_workspace_bytes(const dfp_ortho_desc* d);
+
 /* Output height and width of the forward convolution; DFP_ERR_SHAPE if < 1. */
 dfp_status dfp_output_dims(const dfp_desc* d, int32_t* p, int32_t* q);
 

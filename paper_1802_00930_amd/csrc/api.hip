@@ -656,7 +656,8 @@ const char* dfp_kernel_name(int32_t id) {
       "scale_reset", "amax", "quant_convert", "conv_fwd_valu", "conv_bwd_data_valu", "conv_bwd_wt_valu",
       "weight_prep", "conv_fwd_mfma", "conv_bwd_data_mfma", "conv_bwd_wt_mfma", "bwd_wt_segment_reduce",
       "act_prep", "conv_fwd_i32", "conv_bwd_data_i32", "downconvert_i32", "gemm_prep", "gemm", "quant_blocked", "gemm_blocked",
-      "bn_stats", "bn_finalize", "bn_amax", "bn_convert", "sgd"};
+      "bn_stats", "bn_finalize", "bn_amax", "bn_convert", "sgd",
+      "i8_rows", "i8_transpose", "i8_cols", "i8_gemm", "ortho_norm", "ortho_pack", "ortho_gram", "ortho_poly", "ortho_step"};
   if (id < 0 || id >= K_NUM_KERNELS) return "unknown";
   return names[id];
 }

@@ -34,7 +34,16 @@ enum KernelId : int32_t {
   K_BN_AMAX = 21,
   K_BN_CONVERT = 22,
   K_SGD = 23,
-  K_NUM_KERNELS = 24
+  K_I8_ROWS = 24,
+  K_I8_TRANSPOSE = 25,
+  K_I8_COLS = 26,
+  K_I8_GEMM = 27,
+  K_ORTHO_NORM = 28,
+  K_ORTHO_PACK = 29,
+  K_ORTHO_GRAM = 30,
+  K_ORTHO_POLY = 31,
+  K_ORTHO_STEP = 32,
+  K_NUM_KERNELS = 33
 };
 
 // n / d for 0 <= n < 2^32 by multiply-high (round-up method, l = ceil(log2 d),

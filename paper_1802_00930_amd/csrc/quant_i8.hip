@@ -1,0 +1,399 @@
+// INT8 quantisation with one FP32 scale per row or column (see dfp.h), the
+// operands of the INT8 linear layers.
+//   rows      a row's workgroup (or wave) keeps the row in registers between its
+//             maximum and its rounding: one read, one write
+//   columns   over the tokens of a gradient: partial maxima of slices of the
+//             rows, then the rounding into the transposed layout
+// Both are bound by memory; the exact rounding costs five operations an element.
+#include <algorithm>
+#include <type_traits>
+
+#include "dfp_internal.h"
+#include "dfp_round.h"
+#include "dfp_types.h"
+#include "linear_i8.h"
+
+#pragma clang fp contract(off)
+
+namespace dfp {
+
+namespace {
+
+constexpr int kBlock = 256;
+
+// Scale of a maximum (FP32 bits, NaN and Inf above every finite one): s as
+// stored, and the pair (s, x) is multiplied by `up` before the division so that a
+// subnormal s has all its bits in the reciprocal.
+struct I8Scale {
+  float s, su, inv, up;
+  bool live;
+};
+__device__ __forceinline__ I8Scale i8_scale(uint32_t amax_bits) {
+  I8Scale r;
+  const bool finite = amax_bits < 0x7f800000u;
+  r.s = finite ? __uint_as_float(amax_bits) / 127.f : __uint_as_float(0x7fc00000u);
+  r.live = finite && r.s > 0.f;
+  r.up = r.s < 0x1p-60f ? 0x1p64f : 1.f;
+  r.su = r.s * r.up;
+  r.inv = r.live ? 1.f / r.su : 0.f;
+  return r;
+}
+
+// round(x / s).  x * inv is within one integer of it, and e = x - q s is exact:
+// x and q s are multiples of the ulp of the smaller of x and s, and |e| <= s.
+template <int MODE>
+__device__ __forceinline__ int32_t i8_round(float x, const I8Scale& k, uint32_t u) {
+  const float xu = x * k.up;
+  float q = rintf(xu * k.inv);
+  float e = fmaf(-q, k.su, xu);
+  const float h = 2.f * fabsf(e);
+  const bool move = h > k.su || (h == k.su && ((int32_t)q & 1));
+  const float step = move ? copysignf(1.f, e) : 0.f;
+  q += step;
+  if (MODE == DFP_ROUND_STOCHASTIC) {
+    e = fmaf(-step, k.su, e);
+    const int64_t R = (int64_t)floor((double)(e / k.su) * 0x1p32);
+    q += (float)((int32_t)(R >> 32) + (u < (uint32_t)R ? 1 : 0));
+  }
+  return (int32_t)fminf(fmaxf(q, -127.f), 127.f);
+}
+
+__device__ __forceinline__ uint32_t pack4(int32_t a, int32_t b, int32_t c, int32_t d) {
+  return (a & 0xff) | ((b & 0xff) << 8) | ((c & 0xff) << 16) | ((uint32_t)d << 24);
+}
+
+// Philox words of N consecutive flat indices.
+template <int N>
+__device__ __forceinline__ void words(uint64_t idx, uint32_t k0, uint32_t k1, uint32_t role, uint32_t (&u)[N]) {
+  uint64_t at = ~0ull;
+  uint4 w = make_uint4(0, 0, 0, 0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint64_t q = (idx + i) >> 2;
+    if (q != at) {
+      at = q;
+      w = philox4x32_10(make_uint4((uint32_t)q, (uint32_t)(q >> 32), role, 0u), k0, k1);
+    }
+    const uint32_t s = (uint32_t)(idx + i) & 3;
+    u[i] = s == 0 ? w.x : s == 1 ? w.y : s == 2 ? w.z : w.w;
+  }
+}
+
+template <int MODE>
+__device__ __forceinline__ uint2 i8_round8(const float (&v)[8], const I8Scale& k, uint64_t idx, uint32_t k0,
+                                           uint32_t k1, uint32_t role) {
+  uint32_t u[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (MODE == DFP_ROUND_STOCHASTIC) words<8>(idx, k0, k1, role, u);
+  int32_t q[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) q[i] = i8_round<MODE>(v[i], k, u[i]);
+  const uint2 o = make_uint2(pack4(q[0], q[1], q[2], q[3]), pack4(q[4], q[5], q[6], q[7]));
+  return k.live ? o : make_uint2(0, 0);
+}
+
+// Rows by groups of G threads (64: four rows a workgroup, 256: one), NV vectors of
+// 8 elements a thread in registers; NV = 0: a row of any length, read twice.
+// colw (nullable): every element is first multiplied by its column's weight.
+template <int T, int MODE, int G, int NV, bool WEIGHTED>
+__global__ __launch_bounds__(kBlock) void k_rows_i8(const typename Elem<T>::type* __restrict__ src, int64_t rows,
+                                                    int64_t cols, int64_t ld, const float* __restrict__ colw,
+                                                    int8_t* __restrict__ q, float* __restrict__ scale, uint32_t k0,
+                                                    uint32_t k1, uint32_t role) {
+  __shared__ uint32_t red[kBlock / 64];
+  const int t = threadIdx.x % G;
+  const int64_t per = kBlock / G, nvec = ld / 8;
+  // (every thread of a workgroup makes the same number of rounds)
+  for (int64_t r0 = (int64_t)blockIdx.x * per; r0 < rows; r0 += (int64_t)gridDim.x * per) {
+    const int64_t r = min(r0 + threadIdx.x / G, rows - 1);
+    const bool mine = r0 + threadIdx.x / G < rows;
+    const typename Elem<T>::type* x = src + r * cols;
+    auto load = [&](int64_t c, float (&v)[8]) {
+      load_n<T, 8>(x + c, cols - c, v);
+      if (WEIGHTED) {
+        float w[8];
+        load_n<DFP_F32, 8>(colw + c, cols - c, w);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= w[i];
+      }
+    };
+    uint32_t mx = 0;
+    auto maxof = [&](const float (&v)[8]) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mx = max(mx, __float_as_uint(v[i]) & 0x7fffffffu);
+    };
+    float v[NV > 0 ? NV : 1][8];
+    if constexpr (NV > 0) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) load(((int64_t)t + i * G) * 8, v[i]);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) maxof(v[i]);
+    } else {
+      for (int64_t c = t; c < nvec; c += G) {
+        load(c * 8, v[0]);
+        maxof(v[0]);
+      }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) mx = max(mx, (uint32_t)__shfl_xor((int)mx, o, 64));
+    if constexpr (G > 64) {
+      __syncthreads();
+      if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = mx;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kBlock / 64; ++w) mx = max(mx, red[w]);
+    }
+    const I8Scale k = i8_scale(mx);
+    if (t == 0 && mine) scale[r] = k.s;
+    if constexpr (NV > 0) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int64_t c = (int64_t)t + i * G;
+        if (mine && c < nvec)
+          *reinterpret_cast<uint2*>(q + r * ld + c * 8) = i8_round8<MODE>(v[i], k, r * cols + c * 8, k0, k1, role);
+      }
+    } else {
+      for (int64_t c = t; c < nvec; c += G) {
+        load(c * 8, v[0]);
+        if (mine)
+          *reinterpret_cast<uint2*>(q + r * ld + c * 8) = i8_round8<MODE>(v[0], k, r * cols + c * 8, k0, k1, role);
+      }
+    }
+  }
+}
+
+// 4 x 4 bytes: word i of the result holds byte i of the four words.
+__device__ __forceinline__ void transpose4(const uint32_t (&w)[4], uint32_t (&o)[4]) {
+  const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), b = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u);
+  const uint32_t c = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+  o[0] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+  o[1] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+  o[2] = __builtin_amdgcn_perm(d, c, 0x05040100u);
+  o[3] = __builtin_amdgcn_perm(d, c, 0x07060302u);
+}
+
+// The transposed tile in LDS: 128 columns of 32 words (128 tokens), written out as
+// rows of 128 bytes.  33 words a column keep both directions off shared banks.
+typedef uint32_t TileT[128][33];
+__device__ __forceinline__ void store_tile_t(const TileT& tile, int8_t* qt, int64_t cols, int64_t ldt, int64_t r0,
+                                             int64_t c0) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int c = (threadIdx.x >> 3) + i * 32, w = (threadIdx.x & 7) * 4;
+    if (c0 + c < cols)
+      *reinterpret_cast<uint4*>(qt + (c0 + c) * ldt + r0 + w * 4) =
+          make_uint4(tile[c][w], tile[c][w + 1], tile[c][w + 2], tile[c][w + 3]);
+  }
+}
+
+// INT8 [rows][ld] -> [cols][ldt], zeros for the rows past the last.  128 x 128 tiles.
+__global__ __launch_bounds__(kBlock) void k_transpose_i8(const int8_t* __restrict__ q, int64_t rows, int64_t cols,
+                                                         int64_t ld, int8_t* __restrict__ qt, int64_t ldt,
+                                                         uint32_t ctiles) {
+  __shared__ TileT tile;
+  const int64_t r0 = (int64_t)(blockIdx.x / ctiles) * 128, c0 = (int64_t)(blockIdx.x % ctiles) * 128;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int c4 = threadIdx.x & 31, r4 = (threadIdx.x >> 5) + i * 8;
+    uint32_t w[4], o[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t r = r0 + r4 * 4 + j;
+      w[j] = r < rows ? *reinterpret_cast<const uint32_t*>(q + r * ld + c0 + c4 * 4) : 0u;
+    }
+    transpose4(w, o);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) tile[c4 * 4 + j][r4] = o[j];
+  }
+  __syncthreads();
+  store_tile_t(tile, qt, cols, ldt, r0, c0);
+}
+
+// Column maxima of |x[r][c] roww[r]| and column sums of x over slices of the rows:
+// workgroups of 256 columns by one slice, eight rows at a time.
+template <int T>
+__global__ __launch_bounds__(kBlock) void k_col_max(const typename Elem<T>::type* __restrict__ src, int64_t rows,
+                                                    int64_t cols, const float* __restrict__ roww, int64_t slice,
+                                                    uint32_t cblocks, uint32_t* __restrict__ pmax,
+                                                    float* __restrict__ psum) {
+  __shared__ uint32_t smax[8][256];
+  __shared__ float ssum[8][256];
+  const int cv = threadIdx.x & 31, rg = threadIdx.x >> 5;
+  const int64_t c = (int64_t)(blockIdx.x % cblocks) * 256 + cv * 8, part = blockIdx.x / cblocks;
+  const int64_t r1 = min(rows, (part + 1) * slice);
+  uint32_t mx[8] = {};
+  float sum[8] = {};
+  for (int64_t r = part * slice + rg; r < r1; r += 8) {
+    float v[8];
+    if (c < cols) load_n<T, 8>(src + r * cols + c, cols - c, v);
+    else
+      for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    const float w = roww[r];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      mx[i] = max(mx[i], __float_as_uint(v[i] * w) & 0x7fffffffu);
+      sum[i] += v[i];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    smax[rg][cv * 8 + i] = mx[i];
+    ssum[rg][cv * 8 + i] = sum[i];
+  }
+  __syncthreads();
+  const int64_t oc = (int64_t)(blockIdx.x % cblocks) * 256 + threadIdx.x;
+  uint32_t m = 0;
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    m = max(m, smax[i][threadIdx.x]);
+    s += ssum[i][threadIdx.x];
+  }
+  if (oc < cols) {
+    pmax[part * cols + oc] = m;
+    psum[part * cols + oc] = s;
+  }
+}
+
+// Scales of the columns (and their sums) from the slices, in slice order.
+__global__ __launch_bounds__(kBlock) void k_col_scale(const uint32_t* __restrict__ pmax, const float* __restrict__ psum,
+                                                      int32_t parts, int64_t cols, float* __restrict__ scale,
+                                                      uint32_t* __restrict__ amax, float* __restrict__ sums) {
+  const int64_t c = (int64_t)blockIdx.x * kBlock + threadIdx.x;
+  if (c >= cols) return;
+  uint32_t m = 0;
+  float s = 0.f;
+  for (int32_t p = 0; p < parts; ++p) {
+    m = max(m, pmax[(int64_t)p * cols + c]);
+    s += psum[(int64_t)p * cols + c];
+  }
+  scale[c] = i8_scale(m).s;
+  amax[c] = m;
+  if (sums) sums[c] = s;
+}
+
+// x[r][c] roww[r] rounded by column scale into qt [cols][ldt]: 128 x 128 tiles,
+// a thread 4 rows x 8 columns at a time.
+template <int T, int MODE>
+__global__ __launch_bounds__(kBlock) void k_col_i8_t(const typename Elem<T>::type* __restrict__ src, int64_t rows,
+                                                     int64_t cols, const float* __restrict__ roww,
+                                                     const uint32_t* __restrict__ amax, int8_t* __restrict__ qt,
+                                                     int64_t ldt, uint32_t ctiles, uint32_t k0, uint32_t k1,
+                                                     uint32_t role) {
+  __shared__ TileT tile;
+  const int64_t r0 = (int64_t)(blockIdx.x / ctiles) * 128, c0 = (int64_t)(blockIdx.x % ctiles) * 128;
+  const int c8 = threadIdx.x & 15;
+  const int64_t c = c0 + c8 * 8;
+  I8Scale k[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) k[i] = i8_scale(c + i < cols ? amax[c + i] : 0u);
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r4 = (threadIdx.x >> 4) + h * 16;
+    uint32_t o[8] = {};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int64_t r = r0 + r4 * 4 + j;
+      if (r >= rows || c >= cols) continue;
+      float v[8];
+      load_n<T, 8>(src + r * cols + c, cols - c, v);
+      const float w = roww[r];
+      uint32_t u[8] = {};
+      if (MODE == DFP_ROUND_STOCHASTIC) words<8>(r * cols + c, k0, k1, role, u);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (k[i].live) o[i] |= (uint32_t)(i8_round<MODE>(v[i] * w, k[i], u[i]) & 0xff) << (8 * j);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) tile[c8 * 8 + i][r4] = o[i];
+  }
+  __syncthreads();
+  store_tile_t(tile, qt, cols, ldt, r0, c0);
+}
+
+template <class F>
+dfp_status with_mode(int32_t rounding, F f) {
+  if (rounding == DFP_ROUND_STOCHASTIC) return f(std::integral_constant<int, DFP_ROUND_STOCHASTIC>());
+  return f(std::integral_constant<int, DFP_ROUND_NEAREST>());
+}
+
+constexpr int64_t kMaxBlocks = 1 << 22;  // of a grid-stride launch
+
+}  // namespace
+
+dfp_status launch_rows_i8(int32_t type, int32_t rounding, uint64_t seed, uint32_t role, const void* src, int64_t rows,
+                          int64_t cols, const float* colw, int8_t* q, float* scale, hipStream_t st) {
+  const int64_t ld = i8_ld(cols), nvec = ld / 8;
+  const uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
+  return with_type(type, [&](auto tc) -> dfp_status {
+    constexpr int T = decltype(tc)::value;
+    return with_mode(rounding, [&](auto mc) -> dfp_status {
+      constexpr int MODE = decltype(mc)::value;
+      auto go = [&](auto g, auto nv, auto weighted) -> dfp_status {
+        constexpr int G = decltype(g)::value;
+        const int64_t blocks = std::min<int64_t>((rows + kBlock / G - 1) / (kBlock / G), kMaxBlocks);
+        DFP_LAUNCH(K_I8_ROWS, (k_rows_i8<T, MODE, G, decltype(nv)::value, decltype(weighted)::value>),
+                   dim3((unsigned)blocks), dim3(kBlock), 0, st, (const typename Elem<T>::type*)src, rows, cols, ld,
+                   colw, q, scale, k0, k1, role);
+        return DFP_OK;
+      };
+      auto by_len = [&](auto weighted) -> dfp_status {
+        typedef std::integral_constant<int, 64> Wave;
+        typedef std::integral_constant<int, 256> Group;
+        // the shortest register row that holds it: a wave up to 1024, a workgroup up to 16384
+        if (nvec <= 64) return go(Wave(), std::integral_constant<int, 1>(), weighted);
+        if (nvec <= 128) return go(Wave(), std::integral_constant<int, 2>(), weighted);
+        if (nvec <= 256) return go(Group(), std::integral_constant<int, 1>(), weighted);
+        if (nvec <= 512) return go(Group(), std::integral_constant<int, 2>(), weighted);
+        if (nvec <= 1024) return go(Group(), std::integral_constant<int, 4>(), weighted);
+        if (nvec <= 2048) return go(Group(), std::integral_constant<int, 8>(), weighted);
+        return go(Group(), std::integral_constant<int, 0>(), weighted);
+      };
+      return colw ? by_len(std::true_type()) : by_len(std::false_type());
+    });
+  });
+}
+
+dfp_status launch_transpose_i8(const int8_t* q, int64_t rows, int64_t cols, int8_t* qt, hipStream_t st) {
+  const int64_t rt = (rows + 127) / 128, ct = (cols + 127) / 128;
+  DFP_LAUNCH(K_I8_TRANSPOSE, k_transpose_i8, dim3((unsigned)(rt * ct)), dim3(kBlock), 0, st, q, rows, cols, i8_ld(cols),
+             qt, i8_ld(rows), (uint32_t)ct);
+  return DFP_OK;
+}
+
+ColPlan plan_cols_i8(int64_t rows, int64_t cols) {
+  ColPlan p;
+  const int64_t cb = (cols + 255) / 256;
+  // enough slices for four workgroups a CU, of at least 64 rows
+  int64_t parts = std::max<int64_t>(1, std::min<int64_t>((rows + 63) / 64, 1024 / cb));
+  p.slice = (rows + parts - 1) / parts;
+  p.parts = (rows + p.slice - 1) / p.slice;
+  p.bytes = (p.parts * 2 + 1) * cols * 4;
+  return p;
+}
+
+dfp_status launch_cols_i8_t(int32_t type, int32_t rounding, uint64_t seed, uint32_t role, const void* src,
+                            int64_t rows, int64_t cols, const float* roww, int8_t* qt, float* scale, float* sums,
+                            void* ws, hipStream_t st) {
+  const ColPlan p = plan_cols_i8(rows, cols);
+  uint32_t* pmax = (uint32_t*)ws;
+  float* psum = (float*)(pmax + p.parts * cols);
+  uint32_t* amax = (uint32_t*)(psum + p.parts * cols);
+  const uint32_t cb = (uint32_t)((cols + 255) / 256);
+  const uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
+  const int64_t rt = (rows + 127) / 128, ct = (cols + 127) / 128;
+  return with_type(type, [&](auto tc) -> dfp_status {
+    constexpr int T = decltype(tc)::value;
+    typedef const typename Elem<T>::type* S;
+    DFP_LAUNCH(K_I8_COLS, k_col_max<T>, dim3((unsigned)(cb * p.parts)), dim3(kBlock), 0, st, (S)src, rows, cols, roww,
+               p.slice, cb, pmax, psum);
+    DFP_LAUNCH(K_I8_COLS, k_col_scale, dim3((unsigned)((cols + kBlock - 1) / kBlock)), dim3(kBlock), 0, st, pmax, psum,
+               (int32_t)p.parts, cols, scale, amax, sums);
+    return with_mode(rounding, [&](auto mc) -> dfp_status {
+      DFP_LAUNCH(K_I8_COLS, (k_col_i8_t<T, decltype(mc)::value>), dim3((unsigned)(rt * ct)), dim3(kBlock), 0, st,
+                 (S)src, rows, cols, roww, amax, qt, i8_ld(rows), (uint32_t)ct, k0, k1, role);
+      return DFP_OK;
+    });
+  });
+}
+
+}  // namespace dfp

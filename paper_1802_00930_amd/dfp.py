@@ -51,6 +51,20 @@ class GemmDesc(ctypes.Structure):
                 ("m", "n", "k", "trans_a", "trans_b", "chunk_len", "bits", "path")]
 
 
+class LinearDesc(ctypes.Structure):
+    """Mirror of ``dfp_linear_desc``."""
+    _fields_ = [(name, ctypes.c_int32) for name in ("m", "n", "k", "type", "rounding")] + [("seed", ctypes.c_uint64)]
+
+
+ORTHO_MAX_STEPS = 16
+
+
+class OrthoDesc(ctypes.Structure):
+    """Mirror of ``dfp_ortho_desc``."""
+    _fields_ = [(name, ctypes.c_int32) for name in ("batch", "rows", "cols", "type", "steps")] + \
+        [("eps", ctypes.c_float), ("coef", (ctypes.c_float * 3) * ORTHO_MAX_STEPS)]
+
+
 _lib = None
 
 
@@ -66,7 +80,19 @@ def lib():
         GP = ctypes.POINTER(GemmDesc)
         BP = ctypes.POINTER(BnDesc)
         F = ctypes.c_float
+        LP = ctypes.POINTER(LinearDesc)
+        OP = ctypes.POINTER(OrthoDesc)
         sigs = {
+            "dfp_i8_ld": ([I64], I64),
+            "dfp_quantize_i8": ([I64, I64, I32, I32, ctypes.c_uint64, I32, P, P, P, P, P], I32),
+            "dfp_linear_i8_workspace_bytes": ([LP], SZ),
+            "dfp_gemm_i8": ([LP, P, P, P, P, P, P, P, SZ, P], I32),
+            "dfp_linear_i8_fwd": ([LP, P, P, P, P, P, P, P, P, P, SZ, P], I32),
+            "dfp_linear_i8_bwd_data": ([LP, P, P, P, P, P, SZ, P], I32),
+            "dfp_linear_i8_bwd_weights": ([LP, P, P, P, P, P, P, SZ, P], I32),
+            "dfp_ortho_workspace_bytes": ([OP], SZ),
+            "dfp_orthogonalize": ([OP, P, P, P, SZ, P], I32),
+            "dfp_muon_quantize": ([OP, F, F, F, F, I32, P, P, P, P, P, P, P, SZ, P], I32),
             "dfp_quantize": ([DP, I32, P, P, P, P], I32),
             "dfp_conv_fwd": ([DP, P, P, P, P, P, P, P, SZ, P, P], I32),
             "dfp_conv_bwd_data": ([DP, P, P, P, P, P, P, P, SZ, P, P], I32),
@@ -378,6 +404,160 @@ def dfp_sgd_quantize(lr, mu, wd, bits, rounding, seed, w, v, dw, wq, sw, stream=
     rnd = ROUNDING[rounding] if isinstance(rounding, str) else int(rounding)
     _check("dfp_sgd_quantize", lib().dfp_sgd_quantize(w.numel(), lr, mu, wd, bits, rnd, seed, _ptr(w), _ptr(v),
                                                       _ptr(dw), _ptr(wq), _ptr(sw), _stream(stream)))
+
+
+TYPE_F32, TYPE_BF16, TYPE_F16 = range(3)
+_TYPES = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
+_DTYPES = {code: dtype for dtype, code in _TYPES.items()}
+
+
+def _type(dtype):
+    if dtype not in _TYPES:
+        raise TypeError("%s is not one of %s" % (dtype, ", ".join(map(str, _TYPES))))
+    return _TYPES[dtype]
+
+
+def _need_here(device, *tensors):
+    """Each (tensor, dtype, shape, name): contiguous, of that shape, on the current GPU, where the launch goes."""
+    for t, dtype, shape, what in tensors:
+        if t is None:
+            continue
+        _need(t, dtype, what)
+        if t.shape != shape:
+            raise ValueError("%s must have shape %s, not %s" % (what, tuple(shape), tuple(t.shape)))
+        if t.get_device() != device:
+            raise ValueError("%s is on cuda:%d, the current device is cuda:%d" % (what, t.get_device(), device))
+
+
+def _here(workspace=None):
+    device = torch.cuda.current_device()
+    if workspace is not None and (not workspace.is_contiguous() or workspace.get_device() != device):
+        raise ValueError("workspace must be contiguous and on the current device, cuda:%d" % device)
+    return device
+
+
+def i8_ld(cols: int) -> int:
+    """Bytes of a row of an INT8 operand: cols rounded up to 128."""
+    return int(lib().dfp_i8_ld(cols))
+
+
+def make_linear_desc(m, n, k, dtype=torch.bfloat16, rounding="nearest", seed=0) -> LinearDesc:
+    """y [m, n] = x [m, k] W^T with W [n, k]; x, y and their gradients of `dtype`."""
+    rnd = ROUNDING[rounding] if isinstance(rounding, str) else int(rounding)
+    return LinearDesc(m, n, k, _type(dtype), rnd, seed)
+
+
+def linear_i8_workspace_bytes(d: LinearDesc) -> int:
+    return int(lib().dfp_linear_i8_workspace_bytes(ctypes.byref(d)))
+
+
+def alloc_linear_i8_workspace(d: LinearDesc, device="cuda"):
+    return torch.empty(linear_i8_workspace_bytes(d), dtype=torch.uint8, device=device)
+
+
+def dfp_quantize_i8(src, q, scale, qt=None, rounding="nearest", seed=0, role=ROLE_X, stream=None):
+    """src [rows, cols]; q INT8 [rows, i8_ld(cols)]; scale FP32 [rows]; qt INT8 [cols, i8_ld(rows)]."""
+    code = _type(src.dtype)
+    rows, cols = src.shape
+    _need_here(_here(), (src, src.dtype, (rows, cols), "src"), (q, torch.int8, (rows, i8_ld(cols)), "q"),
+               (scale, torch.float32, (rows,), "scale"), (qt, torch.int8, (cols, i8_ld(rows)), "qt"))
+    rnd = ROUNDING[rounding] if isinstance(rounding, str) else int(rounding)
+    _check("dfp_quantize_i8", lib().dfp_quantize_i8(rows, cols, code, rnd, seed, role, _ptr(src), _ptr(q),
+                                                    _ptr(scale), _ptr(qt), _stream(stream)))
+
+
+def dfp_gemm_i8(d: LinearDesc, a, sa, b, sb, out, bias=None, workspace=None, stream=None):
+    ld = i8_ld(d.k)
+    _need_here(_here(workspace), (a, torch.int8, (d.m, ld), "a"), (sa, torch.float32, (d.m,), "sa"),
+               (b, torch.int8, (d.n, ld), "b"), (sb, torch.float32, (d.n,), "sb"),
+               (bias, torch.float32, (d.n,), "bias"), (out, _DTYPES[d.type], (d.m, d.n), "out"))
+    wp, wn = _ws(workspace)
+    _check("dfp_gemm_i8", lib().dfp_gemm_i8(ctypes.byref(d), _ptr(a), _ptr(sa), _ptr(b), _ptr(sb), _ptr(bias),
+                                            _ptr(out), wp, wn, _stream(stream)))
+
+
+def dfp_linear_i8_fwd(d: LinearDesc, x, wq, sw, y, bias=None, xq=None, sx=None, xqt=None, workspace=None,
+                      stream=None):
+    t, ld = _DTYPES[d.type], i8_ld(d.k)
+    _need_here(_here(workspace), (x, t, (d.m, d.k), "x"), (wq, torch.int8, (d.n, ld), "wq"),
+               (sw, torch.float32, (d.n,), "sw"), (bias, torch.float32, (d.n,), "bias"), (y, t, (d.m, d.n), "y"),
+               (xq, torch.int8, (d.m, ld), "xq"), (sx, torch.float32, (d.m,), "sx"),
+               (xqt, torch.int8, (d.k, i8_ld(d.m)), "xqt"))
+    wp, wn = _ws(workspace)
+    _check("dfp_linear_i8_fwd", lib().dfp_linear_i8_fwd(ctypes.byref(d), _ptr(x), _ptr(wq), _ptr(sw), _ptr(bias),
+                                                        _ptr(y), _ptr(xq), _ptr(sx), _ptr(xqt), wp, wn,
+                                                        _stream(stream)))
+
+
+def dfp_linear_i8_bwd_data(d: LinearDesc, dy, wqt, sw, dx, workspace=None, stream=None):
+    t = _DTYPES[d.type]
+    _need_here(_here(workspace), (dy, t, (d.m, d.n), "dy"), (wqt, torch.int8, (d.k, i8_ld(d.n)), "wqt"),
+               (sw, torch.float32, (d.n,), "sw"), (dx, t, (d.m, d.k), "dx"))
+    wp, wn = _ws(workspace)
+    _check("dfp_linear_i8_bwd_data", lib().dfp_linear_i8_bwd_data(ctypes.byref(d), _ptr(dy), _ptr(wqt), _ptr(sw),
+                                                                  _ptr(dx), wp, wn, _stream(stream)))
+
+
+def dfp_linear_i8_bwd_weights(d: LinearDesc, dy, xqt, sx, dw, db=None, workspace=None, stream=None):
+    _need_here(_here(workspace), (dy, _DTYPES[d.type], (d.m, d.n), "dy"),
+               (xqt, torch.int8, (d.k, i8_ld(d.m)), "xqt"), (sx, torch.float32, (d.m,), "sx"),
+               (dw, torch.float32, (d.n, d.k), "dw"), (db, torch.float32, (d.n,), "db"))
+    wp, wn = _ws(workspace)
+    _check("dfp_linear_i8_bwd_weights",
+           lib().dfp_linear_i8_bwd_weights(ctypes.byref(d), _ptr(dy), _ptr(xqt), _ptr(sx), _ptr(dw), _ptr(db), wp, wn,
+                                           _stream(stream)))
+
+
+def make_ortho_desc(batch, rows, cols, dtype=torch.bfloat16, steps=5, eps=1e-7,
+                    coef=(3.4445, -4.7750, 2.0315)) -> OrthoDesc:
+    """Descriptor of the orthogonalised update; coef: (a, b, c) for every step, or one triple per step."""
+    d = OrthoDesc(batch, rows, cols, _type(dtype), steps, eps)
+    per_step = [coef] * steps if not hasattr(coef[0], "__len__") else list(coef)
+    if len(per_step) != steps or any(len(c) != 3 for c in per_step):
+        raise ValueError("coef must be (a, b, c) or one such triple for each of the %d steps" % steps)
+    for i, c in enumerate(per_step[:ORTHO_MAX_STEPS]):
+        d.coef[i][:] = c
+    return d
+
+
+def ortho_workspace_bytes(d: OrthoDesc) -> int:
+    return int(lib().dfp_ortho_workspace_bytes(ctypes.byref(d)))
+
+
+def alloc_ortho_workspace(d: OrthoDesc, device="cuda"):
+    return torch.empty(ortho_workspace_bytes(d), dtype=torch.uint8, device=device)
+
+
+def _ortho_shapes(d):
+    """The shapes that a descriptor's tensors may have: [batch, rows, cols], or [rows, cols] for one matrix."""
+    return ((d.batch, d.rows, d.cols), (d.rows, d.cols)) if d.batch == 1 else ((d.batch, d.rows, d.cols),)
+
+
+def dfp_orthogonalize(d: OrthoDesc, x, out, workspace=None, stream=None):
+    """x, out [batch, rows, cols] (or [rows, cols] with batch 1) of the descriptor's type; out may be x."""
+    t, shapes = _DTYPES[d.type], _ortho_shapes(d)
+    if x.shape not in shapes:
+        raise ValueError("x must have shape %s, not %s" % (shapes[0], tuple(x.shape)))
+    _need_here(_here(workspace), (x, t, x.shape, "x"), (out, t, x.shape, "out"))
+    wp, wn = _ws(workspace)
+    _check("dfp_orthogonalize", lib().dfp_orthogonalize(ctypes.byref(d), _ptr(x), _ptr(out), wp, wn,
+                                                        _stream(stream)))
+
+
+def dfp_muon_quantize(d: OrthoDesc, lr, mu, wd, scale, w, v, dw, wq=None, sw=None, wqt=None, nesterov=True,
+                      workspace=None, stream=None):
+    """w, v FP32 and dw (the descriptor's type) [batch, rows, cols], or [rows, cols] with batch 1; wq INT8
+    [batch * rows, i8_ld(cols)] and sw FP32 [batch * rows] both or neither; wqt INT8 [cols, i8_ld(rows)], batch 1."""
+    shapes, n = _ortho_shapes(d), d.batch * d.rows
+    if w.shape not in shapes:
+        raise ValueError("w must have shape %s, not %s" % (shapes[0], tuple(w.shape)))
+    _need_here(_here(workspace), (w, torch.float32, w.shape, "w"), (v, torch.float32, w.shape, "v"),
+               (dw, _DTYPES[d.type], w.shape, "dw"), (wq, torch.int8, (n, i8_ld(d.cols)), "wq"),
+               (sw, torch.float32, (n,), "sw"), (wqt, torch.int8, (d.cols, i8_ld(d.rows)), "wqt"))
+    wp, wn = _ws(workspace)
+    _check("dfp_muon_quantize", lib().dfp_muon_quantize(ctypes.byref(d), lr, mu, wd, scale, int(bool(nesterov)),
+                                                        _ptr(w), _ptr(v), _ptr(dw), _ptr(wq), _ptr(sw), _ptr(wqt), wp,
+                                                        wn, _stream(stream)))
 
 
 def alloc_workspace(d: Desc, direction: int, device="cuda"):
