@@ -29,9 +29,10 @@ dfp_status linear_checks(const dfp_linear_desc* d) {
 }
 
 // One workspace serves every call of a descriptor: an INT8 operand, its scales,
-// and what the column maxima of the backward-weights call need.
+// what the column maxima of the backward-weights call need, and the sums of a
+// sliced product.
 struct LinearWs {
-  int64_t op, scale, cols, bytes;
+  int64_t op, scale, cols, slices, bytes;
 };
 LinearWs linear_ws(const dfp_linear_desc& d) {
   LinearWs w;
@@ -44,6 +45,8 @@ LinearWs linear_ws(const dfp_linear_desc& d) {
   w.op = take(std::max({d.m * i8_ld(d.k), d.m * i8_ld(d.n), d.n * i8_ld(d.m)}));
   w.scale = take((int64_t)std::max(d.m, d.n) * 4);
   w.cols = take(plan_cols_i8(d.m, d.n).bytes);
+  w.slices = take(std::max({plan_gemm_i8(d.m, d.n, d.k).bytes, plan_gemm_i8(d.m, d.k, d.n).bytes,
+                            plan_gemm_i8(d.n, d.k, d.m).bytes}));
   w.bytes = at;
   return w;
 }
@@ -102,8 +105,10 @@ dfp_status dfp_gemm_i8(const dfp_linear_desc* d, const int8_t* a, const float* s
   if (!aligned(a, 16) || !aligned(b, 16) || !aligned(out, 16) || !aligned(sa, 4) || !aligned(sb, 4) ||
       !aligned(bias, 4))
     return DFP_ERR_ALIGN;
-  if ((rc = ws_checks(workspace, ws_bytes, linear_ws(*d).bytes)) != DFP_OK) return rc;
-  return launch_gemm_i8(d->m, d->n, d->k, a, sa, b, sb, bias, d->type, out, (hipStream_t)stream);
+  const LinearWs w = linear_ws(*d);
+  if ((rc = ws_checks(workspace, ws_bytes, w.bytes)) != DFP_OK) return rc;
+  return launch_gemm_i8(d->m, d->n, d->k, a, sa, b, sb, bias, d->type, out, (uint8_t*)workspace + w.slices,
+                        (hipStream_t)stream);
 }
 
 dfp_status dfp_linear_i8_fwd(const dfp_linear_desc* d, const void* x, const int8_t* wq, const float* sw,
@@ -122,7 +127,7 @@ dfp_status dfp_linear_i8_fwd(const dfp_linear_desc* d, const void* x, const int8
   int8_t* q = xq ? xq : (int8_t*)workspace + w.op;
   float* s = sx ? sx : (float*)((uint8_t*)workspace + w.scale);
   rc = launch_rows_i8(d->type, d->rounding, d->seed, DFP_ROLE_X, x, d->m, d->k, nullptr, q, s, st);
-  if (rc == DFP_OK) rc = launch_gemm_i8(d->m, d->n, d->k, q, s, wq, sw, bias, d->type, y, st);
+  if (rc == DFP_OK) rc = launch_gemm_i8(d->m, d->n, d->k, q, s, wq, sw, bias, d->type, y, (uint8_t*)workspace + w.slices, st);
   if (rc == DFP_OK && xqt) rc = launch_transpose_i8(q, d->m, d->k, xqt, st);
   return rc;
 }
@@ -140,7 +145,8 @@ dfp_status dfp_linear_i8_bwd_data(const dfp_linear_desc* d, const void* dy, cons
   int8_t* q = (int8_t*)workspace + w.op;
   float* s = (float*)((uint8_t*)workspace + w.scale);
   rc = launch_rows_i8(d->type, d->rounding, d->seed, DFP_ROLE_DY, dy, d->m, d->n, sw, q, s, st);
-  if (rc == DFP_OK) rc = launch_gemm_i8(d->m, d->k, d->n, q, s, wqt, nullptr, nullptr, d->type, dx, st);
+  if (rc == DFP_OK) rc = launch_gemm_i8(d->m, d->k, d->n, q, s, wqt, nullptr, nullptr, d->type, dx,
+                                         (uint8_t*)workspace + w.slices, st);
   return rc;
 }
 
@@ -159,7 +165,8 @@ dfp_status dfp_linear_i8_bwd_weights(const dfp_linear_desc* d, const void* dy, c
   float* s = (float*)((uint8_t*)workspace + w.scale);
   rc = launch_cols_i8_t(d->type, d->rounding, d->seed, DFP_ROLE_DY, dy, d->m, d->n, sx, q, s, db,
                         (uint8_t*)workspace + w.cols, st);
-  if (rc == DFP_OK) rc = launch_gemm_i8(d->n, d->k, d->m, q, s, xqt, nullptr, nullptr, DFP_F32, dw, st);
+  if (rc == DFP_OK) rc = launch_gemm_i8(d->n, d->k, d->m, q, s, xqt, nullptr, nullptr, DFP_F32, dw,
+                                         (uint8_t*)workspace + w.slices, st);
   return rc;
 }
 

@@ -22,8 +22,14 @@ dfp_status launch_cols_i8_t(int32_t type, int32_t rounding, uint64_t seed, uint3
                             int64_t rows, int64_t cols, const float* roww, int8_t* qt, float* scale, float* sums,
                             void* ws, hipStream_t st);
 
-// out [m][n] (type) = (sum over k of a b) sa[m] sb[n] + bias[n]; sb, bias nullable.
+// out [m][n] (type) = (sum over k of a b) sa[m] sb[n] + bias[n]; sb, bias nullable.  ws: plan_gemm_i8(...).bytes.
+struct I8Plan {
+  int32_t side;         // of the output tiles; 0: the kernel for few rows
+  int32_t slices, per;  // of the reduction, pieces in each
+  int64_t bytes;        // the slices' sums
+};
+I8Plan plan_gemm_i8(int64_t m, int64_t n, int64_t k);
 dfp_status launch_gemm_i8(int32_t m, int32_t n, int32_t k, const int8_t* a, const float* sa, const int8_t* b,
-                          const float* sb, const float* bias, int32_t type, void* out, hipStream_t st);
+                          const float* sb, const float* bias, int32_t type, void* out, void* ws, hipStream_t st);
 
 }  // namespace dfp

@@ -1,5 +1,9 @@
 // INT8 products with a scale per row of either operand: out[i][j] =
-// (sum over t of a[i][t] b[j][t]) sa[i] sb[j] + bias[j], the sum exact in INT32.
+// (sum over t of a[i][t] b[j][t]) sa[i] sb[j] + bias[j], the sum exact in INT32,
+// so that it may be cut anywhere and added in any order with the same result.
+//   k_few    few rows (one token, a decoding batch): bound by the weights' bytes
+//   k_tiles  tiles of outputs on the loop of mma_tile.h, the reduction cut into
+//            slices where the tiles alone leave CUs idle; k_slices adds those up
 #include <algorithm>
 #include <type_traits>
 
@@ -18,9 +22,11 @@ struct I8Args {
   const uint8_t *a, *b;
   const float *sa, *sb, *bias;  // sb, bias nullable
   void* out;
-  int64_t ld;  // bytes of an operand row
+  int32_t* part;  // slices: [slice][m][n]
+  int64_t ld;     // bytes of an operand row
   int32_t m, n;
   uint32_t tm, tn;
+  int32_t per;    // pieces of a slice
 };
 
 // One output quad: four consecutive columns j of row i.
@@ -38,36 +44,197 @@ __device__ __forceinline__ void store_quad(const I8Args& g, int64_t i, int64_t j
   store_n<T, 4>((typename Elem<T>::type*)g.out + i * g.n + j, g.n - j, v);
 }
 
-template <int T, int TM, int TN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void k_gemm_i8(I8Args g) {
-  typedef MmaTile<Prod::I8, TM, TN, WM, WN> Tile;
-  __shared__ __align__(16) uint8_t smem[Tile::kLds];
+// grid.y: slices.  SLICED: the sums go to g.part instead.
+template <int T, bool SLICED, int TM, int TN, int WM, int WN, int S>
+__global__ __launch_bounds__(64 * WM * WN, 2) void k_tiles(I8Args g) {
+  typedef MmaTile<Prod::I8, TM, TN, WM, WN, S> Tile;
   uint32_t im, in;
   tile_of(blockIdx.x, g.tm, g.tn, 8, &im, &in);
   const int64_t i0 = (int64_t)im * TM, j0 = (int64_t)in * TN;
+  const int32_t p0 = SLICED ? (int32_t)blockIdx.y * g.per : 0;
+  const int32_t pieces = SLICED ? min(g.per, (int32_t)(g.ld / kPiece) - p0) : (int32_t)(g.ld / kPiece);
   mv4i acc[Tile::FM][Tile::FN];
-  Tile::run(g.a + i0 * g.ld, g.ld, (int32_t)(g.m - i0), g.b + j0 * g.ld, g.ld, (int32_t)(g.n - j0),
-            (int32_t)(g.ld / kPiece), smem, acc);
+  Tile::run(g.a + i0 * g.ld + (int64_t)p0 * kPiece, g.ld, (int32_t)(g.m - i0),
+            g.b + j0 * g.ld + (int64_t)p0 * kPiece, g.ld, (int32_t)(g.n - j0), pieces, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t i1 = i0 + (wave / WN) * (TM / WM) + (lane & 15);
-  const int64_t j1 = j0 + (wave % WN) * (TN / WN) + (lane >> 4) * 4;
+  const int64_t j1 = j0 + (wave % WN) * (TN / WN) + (lane >> 4) * 8;
+  float sa[Tile::FM];
 #pragma unroll
-  for (int i = 0; i < Tile::FM; ++i)
+  for (int i = 0; i < Tile::FM; ++i) sa[i] = SLICED ? 0.f : g.sa[min(i1 + i * 16, (int64_t)g.m - 1)];
 #pragma unroll
-    for (int j = 0; j < Tile::FN; ++j)
-      if (i1 + i * 16 < g.m && j1 + j * 16 < g.n) store_quad<T>(g, i1 + i * 16, j1 + j * 16, acc[i][j]);
+  for (int j = 0; j < Tile::FN; j += 2) {
+    const int64_t jj = j1 + j * 16;
+    float sb[8], bias[8];
+    if (!SLICED && g.sb) load_n<DFP_F32, 8>(g.sb + jj, g.n - jj, sb);
+    if (!SLICED && g.bias) load_n<DFP_F32, 8>(g.bias + jj, g.n - jj, bias);
+#pragma unroll
+    for (int i = 0; i < Tile::FM; ++i) {
+      const int64_t ii = i1 + i * 16;
+      if (ii >= g.m || jj >= g.n) continue;
+      float v[8];
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        const int32_t s = acc[i][j + (r >> 2)][r & 3];
+        if (SLICED) {
+          v[r] = __int_as_float(s);  // stored as it is
+        } else {
+          v[r] = (float)s * sa[i];
+          if (g.sb) v[r] = v[r] * sb[r];
+          if (g.bias) v[r] = v[r] + bias[r];
+        }
+      }
+      if (SLICED)
+        store_n<DFP_F32, 8>((float*)g.part + ((int64_t)blockIdx.y * g.m + ii) * g.n + jj, g.n - jj, v);
+      else
+        store_n<T, 8>((typename Elem<T>::type*)g.out + ii * g.n + jj, g.n - jj, v);
+    }
+  }
 }
+
+// The slices' sums, four columns of a row a thread.
+template <int T>
+__global__ __launch_bounds__(256) void k_slices(I8Args g, int32_t slices) {
+  const int64_t nq = (g.n + 3) / 4, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t i = id / nq, j = id % nq * 4;
+  if (i >= g.m) return;
+  mv4i s = {0, 0, 0, 0};
+  const int32_t* p = g.part + i * g.n + j;
+  for (int32_t k = 0; k < slices; ++k, p += (int64_t)g.m * g.n) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (j + r < g.n) s[r] += p[r];
+  }
+  store_quad<T>(g, i, j, s);
+}
+
+// Few rows.  A workgroup takes 16 columns of up to 16 RT rows over the whole
+// reduction: its waves deal out the pieces among them, every lane reading 16 bytes
+// of a weight row straight into an MFMA operand (no LDS: nothing is read twice),
+// and their sums meet in LDS.
+constexpr int kFewWaves = 8;
+template <int T, int RT, int UNROLL>
+__global__ __launch_bounds__(64 * kFewWaves) void k_few(I8Args g) {
+  __shared__ int32_t part[kFewWaves][RT * 256];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t j0 = (int64_t)blockIdx.x * 16;
+  const int32_t pieces = (int32_t)(g.ld / kPiece);
+  const uint8_t* pb = g.b + min(j0 + (lane & 15), (int64_t)g.n - 1) * g.ld + (lane >> 4) * 16;
+  const uint8_t* pa[RT];
+#pragma unroll
+  for (int i = 0; i < RT; ++i) pa[i] = g.a + (int64_t)min((lane & 15) + i * 16, g.m - 1) * g.ld + (lane >> 4) * 16;
+  mv4i acc[RT];
+#pragma unroll
+  for (int i = 0; i < RT; ++i) acc[i] = mv4i{0, 0, 0, 0};
+  for (int32_t p = wave; p < pieces; p += kFewWaves * UNROLL) {
+    mv4i b[UNROLL][2], a[UNROLL][RT][2];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      const int64_t at = (int64_t)min(p + u * kFewWaves, pieces - 1) * kPiece;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        b[u][h] = *(const mv4i*)(pb + at + h * 64);
+#pragma unroll
+        for (int i = 0; i < RT; ++i) a[u][i][h] = *(const mv4i*)(pa[i] + at + h * 64);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      if (p + u * kFewWaves >= pieces) break;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < RT; ++i) acc[i] = mma16<Prod::I8>(b[u][h], a[u][i][h], acc[i]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < RT; ++i) *(mv4i*)&part[wave][i * 256 + lane * 4] = acc[i];
+  __syncthreads();
+  for (int q = threadIdx.x; q < RT * 64; q += 64 * kFewWaves) {
+    mv4i s = {0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) s += *(const mv4i*)&part[w][q * 4];
+    const int64_t i = (q >> 6) * 16 + (q & 15), j = j0 + ((q >> 4) & 3) * 4;
+    if (i < g.m && j < g.n) store_quad<T>(g, i, j, s);
+  }
+}
+
+// The kernel of a product by an estimate of its time.  A CU takes a piece of a
+// tile alone in `alone` us, and one every `busy` us when it has several tiles at
+// once (measured at 512 x 512 x 8192 and 8192^3: 256 x 256 1.38 and 1.74, 128 x 128
+// 0.57 and 0.58, 64 x 64 0.29 and 0.18).  A slice more means its sums written and
+// read (4 TB/s together) and a second kernel (4 us).
+struct TileKind {
+  int32_t side;
+  double alone, busy;
+};
+constexpr TileKind kKinds[] = {{256, 1.38, 1.74}, {128, 0.57, 0.58}, {64, 0.29, 0.18}};
+constexpr int32_t kFewRows = 64;
+constexpr int64_t kMostPartBytes = 64 << 20;
 
 }  // namespace
 
+I8Plan plan_gemm_i8(int64_t m, int64_t n, int64_t k) {
+  I8Plan best{};
+  if (m <= kFewRows) return best;
+  const int64_t pieces = i8_ld(k) / kPiece;
+  double least = 1e30;
+  for (int t = 0; t < 3; ++t) {
+    const TileKind& kind = kKinds[t];
+    const int64_t tiles = ((m + kind.side - 1) / kind.side) * ((n + kind.side - 1) / kind.side);
+    for (int64_t slices = 1; slices <= 16 && slices <= pieces; slices *= 2) {
+      const int64_t per = (pieces + slices - 1) / slices, used = (pieces + per - 1) / per;
+      const int64_t bytes = used > 1 ? used * m * n * 4 : 0;
+      if (bytes > kMostPartBytes) break;
+      const int64_t a_cu = (tiles * used + 255) / 256;
+      double us = per * std::max(kind.alone, a_cu * kind.busy);
+      if (used > 1) us += 4. + 2. * bytes / 4e6;
+      if (us < least) {
+        least = us;
+        best = {kind.side, (int32_t)used, (int32_t)per, bytes};
+      }
+    }
+  }
+  return best;
+}
+
 dfp_status launch_gemm_i8(int32_t m, int32_t n, int32_t k, const int8_t* a, const float* sa, const int8_t* b,
-                          const float* sb, const float* bias, int32_t type, void* out, hipStream_t st) {
-  I8Args g{(const uint8_t*)a, (const uint8_t*)b, sa, sb, bias, out, i8_ld(k), m, n, 0, 0};
+                          const float* sb, const float* bias, int32_t type, void* out, void* ws, hipStream_t st) {
+  const I8Plan p = plan_gemm_i8(m, n, k);
+  I8Args g{(const uint8_t*)a, (const uint8_t*)b, sa, sb, bias, out, (int32_t*)ws, i8_ld(k), m, n, 0, 0, p.per};
   return with_type(type, [&](auto tc) -> dfp_status {
     constexpr int T = decltype(tc)::value;
-    g.tm = (uint32_t)(((int64_t)m + 127) / 128);
-    g.tn = (uint32_t)(((int64_t)n + 127) / 128);
-    DFP_LAUNCH(K_I8_GEMM, (k_gemm_i8<T, 128, 128, 2, 2>), dim3(g.tm * g.tn), dim3(256), 0, st, g);
+    if (!p.side) {
+      const dim3 grid((unsigned)(((int64_t)n + 15) / 16)), block(64 * kFewWaves);
+      if (m <= 16)
+        DFP_LAUNCH(K_I8_GEMM, (k_few<T, 1, 4>), grid, block, 0, st, g);
+      else if (m <= 32)
+        DFP_LAUNCH(K_I8_GEMM, (k_few<T, 2, 2>), grid, block, 0, st, g);
+      else
+        DFP_LAUNCH(K_I8_GEMM, (k_few<T, 4, 2>), grid, block, 0, st, g);
+      return DFP_OK;
+    }
+    g.tm = (uint32_t)(((int64_t)m + p.side - 1) / p.side);
+    g.tn = (uint32_t)(((int64_t)n + p.side - 1) / p.side);
+    auto tiles = [&](auto sliced) -> dfp_status {
+      constexpr bool SL = decltype(sliced)::value;
+      const dim3 grid(g.tm * g.tn, (unsigned)p.slices);
+      // (a sliced kernel stores integers: one instance serves every type)
+      constexpr int TT = SL ? DFP_F32 : T;
+      if (p.side == 256)
+        DFP_LAUNCH(K_I8_GEMM, (k_tiles<TT, SL, 256, 256, 4, 2, 2>), grid, dim3(512), 0, st, g);
+      else if (p.side == 128)
+        DFP_LAUNCH(K_I8_GEMM, (k_tiles<TT, SL, 128, 128, 2, 2, 2>), grid, dim3(256), 0, st, g);
+      else
+        DFP_LAUNCH(K_I8_GEMM, (k_tiles<TT, SL, 64, 64, 2, 2, 3>), grid, dim3(256), 0, st, g);
+      return DFP_OK;
+    };
+    if (p.slices == 1) return tiles(std::false_type());
+    const dfp_status rc = tiles(std::true_type());
+    if (rc != DFP_OK) return rc;
+    const int64_t quads = (int64_t)m * (((int64_t)n + 3) / 4);
+    DFP_LAUNCH(K_I8_GEMM, k_slices<T>, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, g, p.slices);
     return DFP_OK;
   });
 }

@@ -11,6 +11,9 @@
 // loop over pieces serves them.
 #pragma once
 
+#include <type_traits>
+#include <utility>
+
 #include "dfp_internal.h"
 
 namespace dfp {
@@ -42,85 +45,100 @@ __device__ __forceinline__ typename MmaTypes<P>::acc_t mma16(const mv4i& rows, c
 
 constexpr int kPiece = 128;  // bytes of a row per step of the loop
 
+typedef __attribute__((address_space(3))) void* mma_lds_t;
+
 // One workgroup's TM x TN tile by WM x WN waves.  Lane l of wave (wm, wn) ends
-// with acc[i][j][r] = D[wm TM/WM + 16 i + l % 16][wn TN/WN + 16 j + 4 (l / 16) + r]:
-// four consecutive columns of one row (the B rows are the MFMA's first operand).
-template <Prod P, int TM, int TN, int WM, int WN>
+// with acc[i][j][r] = D[wm TM/WM + 16 i + l % 16][wn TN/WN + 32 (j / 2) + 8 (l / 16) +
+// 4 (j % 2) + r]: of a pair of j, eight consecutive columns of one row, 16 bytes of
+// a 16-bit output (the B rows are the MFMA's first operand, and lane x of a
+// fragment reads row 8 (x / 4) + x % 4 of its 32, four further on for odd j).
+//
+// A ring of S LDS stages: the piece S - 1 ahead goes straight to LDS (16 bytes a
+// lane) while the MFMAs run on this one, with one barrier a piece.  The stages
+// are arrays of their own, not parts of one, so that the compiler sees that a
+// stage's reads do not wait for the loads into the others.  A row's 16-byte quads
+// are permuted by an XOR with three bits of the row, at the source address since
+// the LDS side of such a load is linear: row bits 0 - 2 for A, 0, 1 and 3 for B,
+// which differ in the eight rows that are read at once: no bank conflicts.
+// 8192 x 8192 outputs, 8192 bytes a row, 256 x 256 tiles by 4 x 2 waves: I8 2350
+// TOP/s, F16 1180 TFLOP/s, F16X2 1440 (its 3 products; the MFMAs run 54 and 68 % of
+// the cycles, at 2.07 GHz).  Staging through registers reaches 2240, 1110 and 1210,
+// 128 x 128 outputs a wave (one wave a SIMD) 1840; two groups of waves that
+// take turns between reads and MFMAs, four barriers a piece, 2070.
+template <Prod P, int TM, int TN, int WM, int WN, int S>
 struct MmaTile {
   typedef typename MmaTypes<P>::acc_t acc_t;
   static constexpr int kThreads = 64 * WM * WN;
   static constexpr int FM = TM / WM / 16, FN = TN / WN / 16;
-  static constexpr int kLoadsA = TM * 8 / kThreads, kLoadsB = TN * 8 / kThreads;  // 16-byte pieces of a thread
+  static constexpr int kLoadsA = TM * 8 / kThreads, kLoadsB = TN * 8 / kThreads;  // 16-byte quads of a thread
   static constexpr int kStage = (TM + TN) * kPiece;
-  static constexpr int kLds = 2 * kStage;
   static_assert(TM * 8 % kThreads == 0 && TN * 8 % kThreads == 0, "whole loads");
+  // (kThreads / 8 rows a load, a multiple of 16: a thread's rows have one permutation)
+  static_assert(kThreads % 128 == 0 && FN % 2 == 0, "row bits 0 - 3 of a thread's loads; pairs of j");
+
+  template <class F, int... I>
+  static __device__ __forceinline__ void for_each(F f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>()), ...);
+  }
+  template <class F>
+  static __device__ __forceinline__ void for_stages(F f) {
+    for_each(f, std::make_integer_sequence<int, S>());
+  }
+  template <int I>
+  static __device__ __forceinline__ uint8_t* stage() {
+    __shared__ __align__(16) uint8_t s[kStage];
+    return s;
+  }
 
   // a, b: the tile's first rows; rows past na, nb (counted from there) repeat the
-  // last one, what comes of them is for the caller to drop.  pieces >= 1.
-  // Two LDS stages: while the MFMAs run on one, the next step's rows are on their
-  // way into registers; they are stored once this step's reads are done.  A row's
-  // 16-byte quads are permuted by (quad ^ row % 8), which spreads the 16 rows that
-  // an operand read takes over all banks.
-  static __device__ __forceinline__ void run(const uint8_t* __restrict__ a, int64_t lda, int32_t na,
-                                             const uint8_t* __restrict__ b, int64_t ldb, int32_t nb, int32_t pieces,
-                                             uint8_t* smem, acc_t (&acc)[FM][FN]) {
+  // last one, what comes of them is for the caller to drop.  pieces >= 1; a tile's
+  // rows span less than 2^31 bytes.
+  static __device__ __forceinline__ void run(const uint8_t* a, int64_t lda, int32_t na, const uint8_t* b, int64_t ldb,
+                                             int32_t nb, int32_t pieces, acc_t (&acc)[FM][FN]) {
     const int t = threadIdx.x;
-    const int lane = t & 63, wave = t >> 6;
+    const int lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int wm = wave / WN, wn = wave % WN;
-    uint32_t offa[kLoadsA], offb[kLoadsB];
+    int32_t offa[kLoadsA], offb[kLoadsB];
+    const int row = t >> 3;
+    const int32_t qa16 = ((t & 7) ^ (row & 7)) * 16, qb16 = ((t & 7) ^ ((row & 3) | ((row >> 1) & 4))) * 16;
 #pragma unroll
-    for (int i = 0; i < kLoadsA; ++i)
-      offa[i] = (uint32_t)(min((t >> 3) + i * (kThreads / 8), na - 1) * lda) + (t & 7) * 16;
+    for (int i = 0; i < kLoadsA; ++i) offa[i] = (int32_t)(min(row + i * (kThreads / 8), na - 1) * lda) + qa16;
 #pragma unroll
-    for (int i = 0; i < kLoadsB; ++i)
-      offb[i] = (uint32_t)(min((t >> 3) + i * (kThreads / 8), nb - 1) * ldb) + (t & 7) * 16;
-    // (kThreads / 8 is a multiple of 8: a thread's rows have one permutation)
-    const uint32_t st = (t >> 3) * kPiece + (((t & 7) ^ ((t >> 3) & 7)) << 4);
+    for (int i = 0; i < kLoadsB; ++i) offb[i] = (int32_t)(min(row + i * (kThreads / 8), nb - 1) * ldb) + qb16;
+    const __amdgpu_buffer_rsrc_t ra =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a), (short)0, 0x7fffffff, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rb =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(b), (short)0, 0x7fffffff, 0x00020000);
     const int r = lane & 15, g = lane >> 4;
     const uint32_t fa = (wm * (TM / WM) + r) * kPiece + ((g ^ (r & 7)) << 4);
-    const uint32_t fb = TM * kPiece + (wn * (TN / WN) + r) * kPiece + ((g ^ (r & 7)) << 4);
-
-    mv4i ra[kLoadsA], rb[kLoadsB];
-    auto fetch = [&](int32_t p) {
-      const uint8_t* pa = a + (int64_t)p * kPiece;
-      const uint8_t* pb = b + (int64_t)p * kPiece;
-#pragma unroll
-      for (int i = 0; i < kLoadsA; ++i) ra[i] = *(const mv4i*)(pa + offa[i]);
-#pragma unroll
-      for (int i = 0; i < kLoadsB; ++i) rb[i] = *(const mv4i*)(pb + offb[i]);
-    };
-    auto store = [&](uint32_t stage) {
-      uint8_t* d = smem + stage + st;
-#pragma unroll
-      for (int i = 0; i < kLoadsA; ++i) *(mv4i*)(d + i * (kThreads / 8) * kPiece) = ra[i];
-#pragma unroll
-      for (int i = 0; i < kLoadsB; ++i) *(mv4i*)(d + TM * kPiece + i * (kThreads / 8) * kPiece) = rb[i];
-    };
-
+    // B: row 8 (r / 4) + r % 4, whose permutation bits are r's own 0 - 2
+    const uint32_t fb = TM * kPiece + (wn * (TN / WN) + (r >> 2) * 8 + (r & 3)) * kPiece + ((g ^ (r & 7)) << 4);
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j) acc[i][j] = acc_t{0, 0, 0, 0};
 
-    fetch(0);
-    store(0);
-    if (pieces > 1) fetch(1);
-    __syncthreads();
-    for (int32_t p = 0; p < pieces; ++p) {
-      const uint32_t stage = (p & 1) * kStage;
-      const uint8_t* sa = smem + stage + fa;
-      const uint8_t* sb = smem + stage + fb;
+    auto fetch = [&](int32_t p, uint8_t* s) {
+#pragma unroll
+      for (int i = 0; i < kLoadsA; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (mma_lds_t)(s + (i * kThreads + wave * 64) * 16), 16, offa[i],
+                                                 p * kPiece, 0, 0);
+#pragma unroll
+      for (int i = 0; i < kLoadsB; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (mma_lds_t)(s + TM * kPiece + (i * kThreads + wave * 64) * 16),
+                                                 16, offb[i], p * kPiece, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);  // not behind the reads of the other stage
+    };
+    auto compute = [&](const uint8_t* s) {
       mv4i qa[2][FM], qb[2][FN];
       // quads g and 4 + g of every row: the second is the first with bit 6 turned
       auto read_a = [&](int h) {
 #pragma unroll
-        for (int i = 0; i < FM; ++i)
-          qa[h][i] = *(const mv4i*)(smem + (((uint32_t)(sa - smem)) ^ (h * 64)) + i * 16 * kPiece);
+        for (int i = 0; i < FM; ++i) qa[h][i] = *(const mv4i*)(s + (fa ^ (h * 64)) + i * 16 * kPiece);
       };
       auto read_b = [&](int h) {
 #pragma unroll
-        for (int j = 0; j < FN; ++j)
-          qb[h][j] = *(const mv4i*)(smem + (((uint32_t)(sb - smem)) ^ (h * 64)) + j * 16 * kPiece);
+        for (int j = 0; j < FN; ++j) qb[h][j] = *(const mv4i*)(s + (fb ^ (h * 64)) + ((j >> 1) * 32 + (j & 1) * 4) * kPiece);
       };
       auto product = [&](int ha, int hb) {
 #pragma unroll
@@ -142,12 +160,29 @@ struct MmaTile {
         read_b(1);
         product(1, 1);
       }
-      if (p + 1 < pieces) {
-        store(kStage - stage);
-        if (p + 2 < pieces) fetch(p + 2);
-      }
-      __syncthreads();
-    }
+    };
+
+    // Past the last piece the loads repeat it, into stages that nothing reads any
+    // more: the number in flight stays the same.
+    auto step = [&](int32_t q, auto at) {
+      constexpr int I = decltype(at)::value;
+      __builtin_amdgcn_sched_barrier(0);
+      // This wave's loads of piece q have landed, then everybody's, and everybody is
+      // done reading q - 1.  (As assembly: the compiler's barrier would wait for
+      // every load in flight.)
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S - 2) * (kLoadsA + kLoadsB)) : "memory");
+      fetch(min(q + S - 1, pieces - 1), stage<(I + S - 1) % S>());
+      compute(stage<I>());
+    };
+    for_stages([&](auto at) {
+      constexpr int I = decltype(at)::value;
+      if constexpr (I < S - 1) fetch(min(I, pieces - 1), stage<I>());
+    });
+    for (int32_t q = 0; q < pieces; q += S)
+      for_stages([&](auto at) {
+        if (q + decltype(at)::value < pieces) step(q + decltype(at)::value, at);
+      });
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   }
 };
 

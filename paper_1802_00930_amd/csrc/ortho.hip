@@ -102,16 +102,32 @@ __device__ __forceinline__ void put4(uint8_t* p, int64_t k, const float (&v)[4])
   if (P == Prod::F16X2) d[8] = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
 }
 template <Prod P>
-__device__ __forceinline__ void get4(const uint8_t* p, int64_t k, float (&v)[4]) {
-  const uint2* d = (const uint2*)(p + op_off<P>(k));
-  const uint2 h = d[0];
-  v[0] = h_val(h.x), v[1] = h_val(h.x >> 16), v[2] = h_val(h.y), v[3] = h_val(h.y >> 16);
+__device__ __forceinline__ void put8(uint8_t* p, int64_t k, const float (&v)[8]) {
+  uint32_t hi[4], lo[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const _Float16 a = (_Float16)v[2 * i], b = (_Float16)v[2 * i + 1];
+    hi[i] = h_bits(a) | (uint32_t)h_bits(b) << 16;
+    lo[i] = h_bits((_Float16)(v[2 * i] - (float)a)) | (uint32_t)h_bits((_Float16)(v[2 * i + 1] - (float)b)) << 16;
+  }
+  uint4* d = (uint4*)(p + op_off<P>(k));
+  d[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+  if (P == Prod::F16X2) d[4] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+}
+template <Prod P>
+__device__ __forceinline__ void get8(const uint8_t* p, int64_t k, float (&v)[8]) {
+  const uint4* d = (const uint4*)(p + op_off<P>(k));
+  const uint4 h = d[0];
+  const uint32_t hw[4] = {h.x, h.y, h.z, h.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[2 * i] = h_val(hw[i]), v[2 * i + 1] = h_val(hw[i] >> 16);
   if (P == Prod::F16X2) {
-    const uint2 l = d[8];
-    v[0] += h_val(l.x), v[1] += h_val(l.x >> 16), v[2] += h_val(l.y), v[3] += h_val(l.y >> 16);
+    const uint4 l = d[4];
+    const uint32_t lw[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[2 * i] += h_val(lw[i]), v[2 * i + 1] += h_val(lw[i] >> 16);
   }
 }
-
 // -------------------------------------------------------------------- norm
 // u = x (v null), or the momentum step on v in place and u from it.
 template <int T>
@@ -245,10 +261,9 @@ __device__ __forceinline__ void tri_tile(uint32_t id, uint32_t t, uint32_t* i, u
   *j = row + id;
 }
 
-template <Prod P, int KIND, int T, bool MUON, int TM, int TN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void k_mm(MmArgs g) {
-  typedef MmaTile<P, TM, TN, WM, WN> Tile;
-  __shared__ __align__(16) uint8_t smem[Tile::kLds];
+template <Prod P, int KIND, int T, bool MUON, int TM, int TN, int WM, int WN, int S>
+__global__ __launch_bounds__(64 * WM * WN, 2) void k_mm(MmArgs g) {
+  typedef MmaTile<P, TM, TN, WM, WN, S> Tile;
   const int64_t b = blockIdx.y;
   uint32_t im, in;
   if (KIND == GRAM || KIND == POLY)
@@ -258,24 +273,24 @@ __global__ __launch_bounds__(64 * WM * WN) void k_mm(MmArgs g) {
   const int64_t i0 = (int64_t)im * TM, j0 = (int64_t)in * TN;
   mv4f acc[Tile::FM][Tile::FN];
   Tile::run(g.a + b * g.sa + i0 * g.lda, g.lda, (int32_t)(g.m - i0), g.b + b * g.sb + j0 * g.ldb, g.ldb,
-            (int32_t)(g.n - j0), g.pieces, smem, acc);
+            (int32_t)(g.n - j0), g.pieces, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t i1 = i0 + (wave / WN) * (TM / WM) + (lane & 15);
-  const int64_t j1 = j0 + (wave % WN) * (TN / WN) + (lane >> 4) * 4;
+  const int64_t j1 = j0 + (wave % WN) * (TN / WN) + (lane >> 4) * 8;
 #pragma unroll
-  for (int fi = 0; fi < Tile::FM; ++fi)
+  for (int fj = 0; fj < Tile::FN; fj += 2)
 #pragma unroll
-    for (int fj = 0; fj < Tile::FN; ++fj) {
+    for (int fi = 0; fi < Tile::FM; ++fi) {
       const int64_t i = i1 + fi * 16, j = j1 + fj * 16;
       if (i >= g.m || j >= g.n) continue;
-      float v[4];
+      float v[8];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] = acc[fi][fj][r] * g.unit;
+      for (int r = 0; r < 8; ++r) v[r] = acc[fi][fj + (r >> 2)][r & 3] * g.unit;
       if (KIND == POLY) {
-        float a[4];
-        get4<P>(g.aa + b * g.sr + i * g.ldr, j, a);
+        float a[8];
+        get8<P>(g.aa + b * g.sr + i * g.ldr, j, a);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
+        for (int r = 0; r < 8; ++r) {
           v[r] = fmaf(g.cc, v[r], g.cb * (a[r] * (1.f / (1 << kUnitA))));
           if (i == j + r) {
             g.diag[b * g.rp + i] = v[r];
@@ -285,32 +300,35 @@ __global__ __launch_bounds__(64 * WM * WN) void k_mm(MmArgs g) {
       }
       if (KIND == STEP || KIND == LAST) {
         float* px = g.x32 + (b * g.m + i) * (int64_t)g.n + j;
-        const float4 x = *(const float4*)px;
-        const float xs[4] = {x.x, x.y, x.z, x.w};
+        const float4 x0 = *(const float4*)px, x1 = *(const float4*)(px + 4);
+        const float xs[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = fmaf(g.ca + g.diag[b * g.rp + (g.diag_cols ? j + r : i)], xs[r], v[r]);
-        if (KIND == STEP) *(float4*)px = make_float4(v[0], v[1], v[2], v[3]);
+        for (int r = 0; r < 8; ++r) v[r] = fmaf(g.ca + g.diag[b * g.rp + (g.diag_cols ? j + r : i)], xs[r], v[r]);
+        if (KIND == STEP) {
+          *(float4*)px = make_float4(v[0], v[1], v[2], v[3]);
+          *(float4*)(px + 4) = make_float4(v[4], v[5], v[6], v[7]);
+        }
       }
       if (KIND == LAST) {
         if (i >= g.R || j >= g.C) continue;
         const int64_t at = (b * g.R + i) * g.C + j;
         if (MUON) {
-          float w[4];
-          load_n<DFP_F32, 4>(g.w + at, g.C - j, w);
+          float w[8];
+          load_n<DFP_F32, 8>(g.w + at, g.C - j, w);
 #pragma unroll
-          for (int r = 0; r < 4; ++r) w[r] = fmaf(-g.alpha, v[r], g.keep * w[r]);
-          store_n<DFP_F32, 4>(g.w + at, g.C - j, w);
+          for (int r = 0; r < 8; ++r) w[r] = fmaf(-g.alpha, v[r], g.keep * w[r]);
+          store_n<DFP_F32, 8>(g.w + at, g.C - j, w);
         } else {
-          store_n<T, 4>((typename Elem<T>::type*)g.out + at, g.C - j, v);
+          store_n<T, 8>((typename Elem<T>::type*)g.out + at, g.C - j, v);
         }
         continue;
       }
 #pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] *= g.uout;
-      put4<P>(g.rowop + b * g.sr + i * g.ldr, j, v);
+      for (int r = 0; r < 8; ++r) v[r] *= g.uout;
+      put8<P>(g.rowop + b * g.sr + i * g.ldr, j, v);
       if (KIND == STEP || im != in) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) put1<P>(g.colop + b * g.sc + (j + r) * g.ldc, i, v[r]);
+        for (int r = 0; r < 8; ++r) put1<P>(g.colop + b * g.sc + (j + r) * g.ldc, i, v[r]);
       }
     }
 }
@@ -364,7 +382,7 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
     g.rowop = g.colop = aa;
     g.ldr = g.ldc = p.rp * p.e;
     g.sr = g.sc = ss;
-    DFP_LAUNCH(K_ORTHO_GRAM, (k_mm<P, GRAM, 0, false, TM, TN, 2, 2>), dim3(ts * (ts + 1) / 2, nb), dim3(256), 0, st, g);
+    DFP_LAUNCH(K_ORTHO_GRAM, (k_mm<P, GRAM, 0, false, TM, TN, 2, 2, 2>), dim3(ts * (ts + 1) / 2, nb), dim3(256), 0, st, g);
     // B = b A + c A A
     g.a = g.b = g.aa = aa;
     g.lda = g.ldb = p.rp * p.e;
@@ -373,7 +391,7 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
     g.unit = kInvA * kInvA;
     g.uout = ub;
     g.rowop = g.colop = bb;
-    DFP_LAUNCH(K_ORTHO_POLY, (k_mm<P, POLY, 0, false, TM, TN, 2, 2>), dim3(ts * (ts + 1) / 2, nb), dim3(256), 0, st, g);
+    DFP_LAUNCH(K_ORTHO_POLY, (k_mm<P, POLY, 0, false, TM, TN, 2, 2, 2>), dim3(ts * (ts + 1) / 2, nb), dim3(256), 0, st, g);
     // X = a X + B X, in the caller's orientation: rows of B by rows of X^T, or rows of X by rows of B
     uint8_t *from = step[s & 1], *to = step[(s + 1) & 1];
     g.a = p.tall ? from : bb;
@@ -396,9 +414,9 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
     g.alpha = alpha, g.keep = keep;
     const dim3 grid(g.tm * g.tn, nb);
     if (s + 1 < d.steps)
-      DFP_LAUNCH(K_ORTHO_STEP, (k_mm<P, STEP, 0, false, TM, TN, 2, 2>), grid, dim3(256), 0, st, g);
+      DFP_LAUNCH(K_ORTHO_STEP, (k_mm<P, STEP, 0, false, TM, TN, 2, 2, 2>), grid, dim3(256), 0, st, g);
     else
-      DFP_LAUNCH(K_ORTHO_STEP, (k_mm<P, LAST, T, MUON, TM, TN, 2, 2>), grid, dim3(256), 0, st, g);
+      DFP_LAUNCH(K_ORTHO_STEP, (k_mm<P, LAST, T, MUON, TM, TN, 2, 2, 2>), grid, dim3(256), 0, st, g);
   }
   return DFP_OK;
 }
