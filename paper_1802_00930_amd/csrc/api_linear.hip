@@ -124,6 +124,8 @@ dfp_status dfp_linear_i8_fwd(const dfp_linear_desc* d, const void* x, const int8
   const LinearWs w = linear_ws(*d);
   if ((rc = ws_checks(workspace, ws_bytes, w.bytes)) != DFP_OK) return rc;
   hipStream_t st = (hipStream_t)stream;
+  if (!xq && !sx && !xqt && fits_token_i8(d->m, d->k))
+    return launch_token_i8(d->m, d->n, d->k, d->type, d->rounding, d->seed, x, wq, sw, bias, y, st);
   int8_t* q = xq ? xq : (int8_t*)workspace + w.op;
   float* s = sx ? sx : (float*)((uint8_t*)workspace + w.scale);
   rc = launch_rows_i8(d->type, d->rounding, d->seed, DFP_ROLE_X, x, d->m, d->k, nullptr, q, s, st);

@@ -1,0 +1,90 @@
+// Scale of a row and rounding of its elements to INT8 (see dfp.h).
+#pragma once
+
+#include <type_traits>
+
+#include "dfp_internal.h"
+#include "dfp_round.h"
+
+#pragma clang fp contract(off)
+
+namespace dfp {
+
+// Scale of a maximum (FP32 bits, NaN and Inf above every finite one): s as
+// stored, and the pair (s, x) is multiplied by `up` before the division so that a
+// subnormal s has all its bits in the reciprocal.
+struct I8Scale {
+  float s, su, inv, up;
+  bool live;
+};
+__device__ __forceinline__ I8Scale i8_scale(uint32_t amax_bits) {
+  I8Scale r;
+  const bool finite = amax_bits < 0x7f800000u;
+  r.s = finite ? __uint_as_float(amax_bits) / 127.f : __uint_as_float(0x7fc00000u);
+  r.live = finite && r.s > 0.f;
+  r.up = r.s < 0x1p-60f ? 0x1p64f : 1.f;
+  r.su = r.s * r.up;
+  r.inv = r.live ? 1.f / r.su : 0.f;
+  return r;
+}
+
+// round(x / s).  x * inv is within one integer of it, and e = x - q s is exact:
+// x and q s are multiples of the ulp of the smaller of x and s, and |e| <= s.
+template <int MODE>
+__device__ __forceinline__ int32_t i8_round(float x, const I8Scale& k, uint32_t u) {
+  const float xu = x * k.up;
+  float q = rintf(xu * k.inv);
+  float e = fmaf(-q, k.su, xu);
+  const float h = 2.f * fabsf(e);
+  const bool move = h > k.su || (h == k.su && ((int32_t)q & 1));
+  const float step = move ? copysignf(1.f, e) : 0.f;
+  q += step;
+  if (MODE == DFP_ROUND_STOCHASTIC) {
+    e = fmaf(-step, k.su, e);
+    const int64_t R = (int64_t)floor((double)(e / k.su) * 0x1p32);
+    q += (float)((int32_t)(R >> 32) + (u < (uint32_t)R ? 1 : 0));
+  }
+  return (int32_t)fminf(fmaxf(q, -127.f), 127.f);
+}
+
+__device__ __forceinline__ uint32_t pack4(int32_t a, int32_t b, int32_t c, int32_t d) {
+  return (a & 0xff) | ((b & 0xff) << 8) | ((c & 0xff) << 16) | ((uint32_t)d << 24);
+}
+
+// Philox words of N consecutive flat indices.
+template <int N>
+__device__ __forceinline__ void words(uint64_t idx, uint32_t k0, uint32_t k1, uint32_t role, uint32_t (&u)[N]) {
+  uint64_t at = ~0ull;
+  uint4 w = make_uint4(0, 0, 0, 0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint64_t q = (idx + i) >> 2;
+    if (q != at) {
+      at = q;
+      w = philox4x32_10(make_uint4((uint32_t)q, (uint32_t)(q >> 32), role, 0u), k0, k1);
+    }
+    const uint32_t s = (uint32_t)(idx + i) & 3;
+    u[i] = s == 0 ? w.x : s == 1 ? w.y : s == 2 ? w.z : w.w;
+  }
+}
+
+template <int MODE>
+__device__ __forceinline__ uint2 i8_round8(const float (&v)[8], const I8Scale& k, uint64_t idx, uint32_t k0,
+                                           uint32_t k1, uint32_t role) {
+  uint32_t u[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  if (MODE == DFP_ROUND_STOCHASTIC) words<8>(idx, k0, k1, role, u);
+  int32_t q[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) q[i] = i8_round<MODE>(v[i], k, u[i]);
+  const uint2 o = make_uint2(pack4(q[0], q[1], q[2], q[3]), pack4(q[4], q[5], q[6], q[7]));
+  return k.live ? o : make_uint2(0, 0);
+}
+
+// f(integral_constant of the rounding), for a checked rounding.
+template <class F>
+dfp_status with_mode(int32_t rounding, F f) {
+  if (rounding == DFP_ROUND_STOCHASTIC) return f(std::integral_constant<int, DFP_ROUND_STOCHASTIC>());
+  return f(std::integral_constant<int, DFP_ROUND_NEAREST>());
+}
+
+}  // namespace dfp

@@ -31,5 +31,10 @@ struct I8Plan {
 I8Plan plan_gemm_i8(int64_t m, int64_t n, int64_t k);
 dfp_status launch_gemm_i8(int32_t m, int32_t n, int32_t k, const int8_t* a, const float* sa, const int8_t* b,
                           const float* sb, const float* bias, int32_t type, void* out, void* ws, hipStream_t st);
+// The forward call for a few tokens in one launch, where fits_token_i8.
+bool fits_token_i8(int64_t m, int64_t k);
+dfp_status launch_token_i8(int32_t m, int32_t n, int32_t k, int32_t type, int32_t rounding, uint64_t seed,
+                           const void* x, const int8_t* b, const float* sb, const float* bias, void* out,
+                           hipStream_t st);
 
 }  // namespace dfp

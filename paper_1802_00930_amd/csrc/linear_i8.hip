@@ -9,6 +9,7 @@
 
 #include "dfp_internal.h"
 #include "dfp_types.h"
+#include "i8_round.h"
 #include "linear_i8.h"
 #include "mma_tile.h"
 
@@ -99,11 +100,16 @@ __global__ __launch_bounds__(256) void k_slices(I8Args g, int32_t slices) {
   const int64_t i = id / nq, j = id % nq * 4;
   if (i >= g.m) return;
   mv4i s = {0, 0, 0, 0};
-  const int32_t* p = g.part + i * g.n + j;
-  for (int32_t k = 0; k < slices; ++k, p += (int64_t)g.m * g.n) {
+  const float* p = (const float*)g.part + i * g.n + j;
+  for (int32_t k = 0; k < slices; k += 8) {  // eight loads in flight
+    float v[8][4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-      if (j + r < g.n) s[r] += p[r];
+    for (int u = 0; u < 8; ++u)
+      load_n<DFP_F32, 4>(p + (int64_t)min(k + u, slices - 1) * g.m * g.n, g.n - j, v[u]);
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) s[r] += k + u < slices ? __float_as_int(v[u][r]) : 0;
   }
   store_quad<T>(g, i, j, s);
 }
@@ -113,6 +119,11 @@ __global__ __launch_bounds__(256) void k_slices(I8Args g, int32_t slices) {
 // of a weight row straight into an MFMA operand (no LDS: nothing is read twice),
 // and their sums meet in LDS.
 constexpr int kFewWaves = 8;
+constexpr int kTokenRows = 2;
+constexpr int kTokenVecs = 8;                                        // of 8 elements, a lane's share of a row
+constexpr int kTokenBytes = 64 * 8 * kTokenVecs * kFewWaves + 16 * kTokenRows;  // all waves' rows, and their padding
+// log2 of the waves that share a row of x
+__host__ __device__ __forceinline__ int32_t token_shift(int64_t m) { return m == 1 ? 3 : m == 2 ? 2 : m <= 4 ? 1 : 0; }
 template <int T, int RT, int UNROLL>
 __global__ __launch_bounds__(64 * kFewWaves) void k_few(I8Args g) {
   __shared__ int32_t part[kFewWaves][RT * 256];
@@ -160,11 +171,99 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few(I8Args g) {
   }
 }
 
-// The kernel of a product by an estimate of its time.  A CU takes a piece of a
-// tile alone in `alone` us, and one every `busy` us when it has several tiles at
-// once (measured at 512 x 512 x 8192 and 8192^3: 256 x 256 1.38 and 1.74, 128 x 128
-// 0.57 and 0.58, 64 x 64 0.29 and 0.18).  A slice more means its sums written and
-// read (4 TB/s together) and a second kernel (4 us).
+// One token or a few, quantised on the way: every workgroup of k_few's kind turns
+// the rows of x into INT8 in its own LDS, which takes the launch of a quantiser out
+// of the call.  The first pieces of the weights are requested before.
+template <int T, int MODE, int UNROLL>
+__global__ __launch_bounds__(64 * kFewWaves) void k_token(I8Args g, const typename Elem<T>::type* __restrict__ x,
+                                                          int32_t k, uint32_t k0, uint32_t k1) {
+  __shared__ __align__(16) uint8_t xq[kTokenBytes];
+  __shared__ int32_t part[kFewWaves][256];
+  __shared__ uint32_t red[kFewWaves];
+  __shared__ float sx[kTokenRows];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t j0 = (int64_t)blockIdx.x * 16;
+  const int32_t pieces = (int32_t)(g.ld / kPiece), stride = (int32_t)g.ld + 16;  // 16: rows on other banks
+  const uint8_t* pb = g.b + min(j0 + (lane & 15), (int64_t)g.n - 1) * g.ld + (lane >> 4) * 16;
+  mv4i b[UNROLL][2];
+  auto fetch = [&](int32_t p) {
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        b[u][h] = *(const mv4i*)(pb + (int64_t)min(p + u * kFewWaves, pieces - 1) * kPiece + h * 64);
+  };
+  fetch(wave);
+  // 8, 4, 2 or 1 waves a row; the row stays in registers
+  const int32_t sh = token_shift(g.m), row = wave >> sh, sub = wave & ((1 << sh) - 1);
+  float v[kTokenVecs][8];
+  uint32_t mx = 0;
+#pragma unroll
+  for (int i = 0; i < kTokenVecs; ++i) {
+    const int32_t c = ((i << sh | sub) * 64 + lane) * 8;
+    if (row < g.m && c < k) {
+      load_n<T, 8>(x + (int64_t)row * k + c, k - c, v[i]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < kTokenVecs; ++i)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mx = max(mx, __float_as_uint(v[i][e]) & 0x7fffffffu);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) mx = max(mx, (uint32_t)__shfl_xor((int)mx, o, 64));
+  if (lane == 0) red[wave] = mx;
+  __syncthreads();
+  for (int w = 0; w < 1 << sh; ++w) mx = max(mx, red[(row << sh) + w]);
+  const I8Scale sc = i8_scale(mx);
+  if (sub == 0 && lane == 0) sx[row] = sc.s;
+#pragma unroll
+  for (int i = 0; i < kTokenVecs; ++i) {
+    const int32_t c = ((i << sh | sub) * 64 + lane) * 8;
+    if (row < g.m && c < (int32_t)g.ld)
+      *(uint2*)(xq + row * stride + c) = i8_round8<MODE>(v[i], sc, (int64_t)row * k + c, k0, k1, DFP_ROLE_X);
+  }
+  __syncthreads();
+  const uint8_t* pa = xq + min(lane & 15, g.m - 1) * stride + (lane >> 4) * 16;
+  mv4i acc = {0, 0, 0, 0};
+  for (int32_t p = wave; p < pieces; p += kFewWaves * UNROLL) {
+    mv4i w[UNROLL][2];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) w[u][0] = b[u][0], w[u][1] = b[u][1];
+    if (p + kFewWaves * UNROLL < pieces) fetch(p + kFewWaves * UNROLL);
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      if (p + u * kFewWaves >= pieces) break;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        acc = mma16<Prod::I8>(w[u][h], *(const mv4i*)(pa + (p + u * kFewWaves) * kPiece + h * 64), acc);
+    }
+  }
+  *(mv4i*)&part[wave][lane * 4] = acc;
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    mv4i s = {0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < kFewWaves; ++w) s += *(const mv4i*)&part[w][lane * 4];
+    const int64_t i = lane & 15, j = j0 + (lane >> 4) * 4;
+    g.sa = sx;
+    if (i < g.m && j < g.n) store_quad<T>(g, i, j, s);
+  }
+}
+
+// The kernel of a product by an estimate of its time (us).
+//   k_few    a CU takes 0.15, 0.21 or 0.35 for a piece of 16 columns by up to 16, 32
+//            or 64 rows (4096 x 4096, 8192 x 2048 and 8192 x 8192 weights).
+//   k_tiles  a piece of a tile takes `alone` if a CU has one tile and `busy` a tile
+//            if it has several (512 x 512 x 8192 and 8192^3); with weights that come
+//            from memory, as they do for few rows, a quarter more.  Slices mean that
+//            their sums are written and read (4 TB/s) and a second kernel (4).
+// At 64 rows: 4096 x 4096 k_few 13.8, tiles 12.7; 8192 x 2048 13.4 and 9.2; 8192 x
+// 8192 44 and 22; 1024 x 1024 5.0 and 5.2.  At 24: 9.6 and 13.6; 8.5 and 8.8; 25.5 and
+// 18.8; 3.6 and 4.8.
 struct TileKind {
   int32_t side;
   double alone, busy;
@@ -177,9 +276,12 @@ constexpr int64_t kMostPartBytes = 64 << 20;
 
 I8Plan plan_gemm_i8(int64_t m, int64_t n, int64_t k) {
   I8Plan best{};
-  if (m <= kFewRows) return best;
   const int64_t pieces = i8_ld(k) / kPiece;
   double least = 1e30;
+  if (m <= kFewRows) {
+    least = 2. + ((n + 15) / 16 + 255) / 256 * pieces * (m <= 16 ? 0.15 : m <= 32 ? 0.21 : 0.35);
+    if (m <= 16) return best;
+  }
   for (int t = 0; t < 3; ++t) {
     const TileKind& kind = kKinds[t];
     const int64_t tiles = ((m + kind.side - 1) / kind.side) * ((n + kind.side - 1) / kind.side);
@@ -188,7 +290,7 @@ I8Plan plan_gemm_i8(int64_t m, int64_t n, int64_t k) {
       const int64_t bytes = used > 1 ? used * m * n * 4 : 0;
       if (bytes > kMostPartBytes) break;
       const int64_t a_cu = (tiles * used + 255) / 256;
-      double us = per * std::max(kind.alone, a_cu * kind.busy);
+      double us = 2.5 + per * std::max(kind.alone, a_cu * kind.busy) * (m <= kFewRows ? 1.25 : 1.);
       if (used > 1) us += 4. + 2. * bytes / 4e6;
       if (us < least) {
         least = us;
@@ -197,6 +299,25 @@ I8Plan plan_gemm_i8(int64_t m, int64_t n, int64_t k) {
     }
   }
   return best;
+}
+
+bool fits_token_i8(int64_t m, int64_t k) {
+  return m <= kTokenRows && i8_ld(k) <= (int64_t)64 * 8 * kTokenVecs << token_shift(m);
+}
+
+dfp_status launch_token_i8(int32_t m, int32_t n, int32_t k, int32_t type, int32_t rounding, uint64_t seed,
+                           const void* x, const int8_t* b, const float* sb, const float* bias, void* out,
+                           hipStream_t st) {
+  I8Args g{nullptr, (const uint8_t*)b, nullptr, sb, bias, out, nullptr, i8_ld(k), m, n, 0, 0, 0};
+  return with_type(type, [&](auto tc) -> dfp_status {
+    constexpr int T = decltype(tc)::value;
+    return with_mode(rounding, [&](auto mc) -> dfp_status {
+      DFP_LAUNCH(K_I8_GEMM, (k_token<T, decltype(mc)::value, 4>), dim3((unsigned)(((int64_t)n + 15) / 16)),
+                 dim3(64 * kFewWaves), 0, st, g, (const typename Elem<T>::type*)x, k, (uint32_t)seed,
+                 (uint32_t)(seed >> 32));
+      return DFP_OK;
+    });
+  });
 }
 
 dfp_status launch_gemm_i8(int32_t m, int32_t n, int32_t k, const int8_t* a, const float* sa, const int8_t* b,
@@ -210,9 +331,9 @@ dfp_status launch_gemm_i8(int32_t m, int32_t n, int32_t k, const int8_t* a, cons
       if (m <= 16)
         DFP_LAUNCH(K_I8_GEMM, (k_few<T, 1, 4>), grid, block, 0, st, g);
       else if (m <= 32)
-        DFP_LAUNCH(K_I8_GEMM, (k_few<T, 2, 2>), grid, block, 0, st, g);
+        DFP_LAUNCH(K_I8_GEMM, (k_few<T, 2, 4>), grid, block, 0, st, g);
       else
-        DFP_LAUNCH(K_I8_GEMM, (k_few<T, 4, 2>), grid, block, 0, st, g);
+        DFP_LAUNCH(K_I8_GEMM, (k_few<T, 4, 4>), grid, block, 0, st, g);
       return DFP_OK;
     }
     g.tm = (uint32_t)(((int64_t)m + p.side - 1) / p.side);

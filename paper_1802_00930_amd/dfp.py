@@ -417,28 +417,39 @@ def _type(dtype):
     return _TYPES[dtype]
 
 
-def _need_here(device, *tensors):
-    """Each (tensor, dtype, shape, name): contiguous, of that shape, on the current GPU, where the launch goes."""
+def _refuse(device, t, dtype, shape, what):
+    _need(t, dtype, what)
+    if t.shape != shape:
+        raise ValueError("%s must have shape %s, not %s" % (what, tuple(shape), tuple(t.shape)))
+    raise ValueError("%s is on cuda:%d, the current device is cuda:%d" % (what, t.get_device(), device))
+
+
+def _here(workspace, *tensors):
+    """Checks each (tensor or None, dtype, shape, name): contiguous, of that shape, on the current GPU, where the
+    launch goes.  Returns the workspace's pointer and bytes and the tensors' pointers."""
+    device = _device() if _device else torch.cuda.current_device()
+    out = [None, 0]
+    if workspace is not None:
+        if not workspace.is_contiguous() or workspace.get_device() != device:
+            raise ValueError("workspace must be contiguous and on the current device, cuda:%d" % device)
+        out = [workspace.data_ptr(), workspace.nbytes]
     for t, dtype, shape, what in tensors:
         if t is None:
+            out.append(None)
             continue
-        _need(t, dtype, what)
-        if t.shape != shape:
-            raise ValueError("%s must have shape %s, not %s" % (what, tuple(shape), tuple(t.shape)))
-        if t.get_device() != device:
-            raise ValueError("%s is on cuda:%d, the current device is cuda:%d" % (what, t.get_device(), device))
-
-
-def _here(workspace=None):
-    device = torch.cuda.current_device()
-    if workspace is not None and (not workspace.is_contiguous() or workspace.get_device() != device):
-        raise ValueError("workspace must be contiguous and on the current device, cuda:%d" % device)
-    return device
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+            _refuse(device, t, dtype, shape, what)
+        out.append(t.data_ptr())
+    return out
 
 
 def i8_ld(cols: int) -> int:
     """Bytes of a row of an INT8 operand: cols rounded up to 128."""
     return int(lib().dfp_i8_ld(cols))
+
+
+def _ld(cols):
+    return (cols + 127) & ~127
 
 
 def make_linear_desc(m, n, k, dtype=torch.bfloat16, rounding="nearest", seed=0) -> LinearDesc:
@@ -459,53 +470,49 @@ def dfp_quantize_i8(src, q, scale, qt=None, rounding="nearest", seed=0, role=ROL
     """src [rows, cols]; q INT8 [rows, i8_ld(cols)]; scale FP32 [rows]; qt INT8 [cols, i8_ld(rows)]."""
     code = _type(src.dtype)
     rows, cols = src.shape
-    _need_here(_here(), (src, src.dtype, (rows, cols), "src"), (q, torch.int8, (rows, i8_ld(cols)), "q"),
-               (scale, torch.float32, (rows,), "scale"), (qt, torch.int8, (cols, i8_ld(rows)), "qt"))
+    _, _, ps, pq, psc, pqt = _here(None, (src, src.dtype, (rows, cols), "src"), (q, torch.int8, (rows, _ld(cols)), "q"),
+                                   (scale, torch.float32, (rows,), "scale"),
+                                   (qt, torch.int8, (cols, _ld(rows)), "qt"))
     rnd = ROUNDING[rounding] if isinstance(rounding, str) else int(rounding)
-    _check("dfp_quantize_i8", lib().dfp_quantize_i8(rows, cols, code, rnd, seed, role, _ptr(src), _ptr(q),
-                                                    _ptr(scale), _ptr(qt), _stream(stream)))
+    _check("dfp_quantize_i8", lib().dfp_quantize_i8(rows, cols, code, rnd, seed, role, ps, pq, psc, pqt,
+                                                    _stream(stream)))
 
 
 def dfp_gemm_i8(d: LinearDesc, a, sa, b, sb, out, bias=None, workspace=None, stream=None):
-    ld = i8_ld(d.k)
-    _need_here(_here(workspace), (a, torch.int8, (d.m, ld), "a"), (sa, torch.float32, (d.m,), "sa"),
-               (b, torch.int8, (d.n, ld), "b"), (sb, torch.float32, (d.n,), "sb"),
-               (bias, torch.float32, (d.n,), "bias"), (out, _DTYPES[d.type], (d.m, d.n), "out"))
-    wp, wn = _ws(workspace)
-    _check("dfp_gemm_i8", lib().dfp_gemm_i8(ctypes.byref(d), _ptr(a), _ptr(sa), _ptr(b), _ptr(sb), _ptr(bias),
-                                            _ptr(out), wp, wn, _stream(stream)))
+    m, n, ld = d.m, d.n, _ld(d.k)
+    wp, wn, pa, psa, pb, psb, pbias, po = _here(
+        workspace, (a, torch.int8, (m, ld), "a"), (sa, torch.float32, (m,), "sa"), (b, torch.int8, (n, ld), "b"),
+        (sb, torch.float32, (n,), "sb"), (bias, torch.float32, (n,), "bias"), (out, _DTYPES[d.type], (m, n), "out"))
+    _check("dfp_gemm_i8", lib().dfp_gemm_i8(d, pa, psa, pb, psb, pbias, po, wp, wn, _stream(stream)))
 
 
 def dfp_linear_i8_fwd(d: LinearDesc, x, wq, sw, y, bias=None, xq=None, sx=None, xqt=None, workspace=None,
                       stream=None):
-    t, ld = _DTYPES[d.type], i8_ld(d.k)
-    _need_here(_here(workspace), (x, t, (d.m, d.k), "x"), (wq, torch.int8, (d.n, ld), "wq"),
-               (sw, torch.float32, (d.n,), "sw"), (bias, torch.float32, (d.n,), "bias"), (y, t, (d.m, d.n), "y"),
-               (xq, torch.int8, (d.m, ld), "xq"), (sx, torch.float32, (d.m,), "sx"),
-               (xqt, torch.int8, (d.k, i8_ld(d.m)), "xqt"))
-    wp, wn = _ws(workspace)
-    _check("dfp_linear_i8_fwd", lib().dfp_linear_i8_fwd(ctypes.byref(d), _ptr(x), _ptr(wq), _ptr(sw), _ptr(bias),
-                                                        _ptr(y), _ptr(xq), _ptr(sx), _ptr(xqt), wp, wn,
+    m, n, k, t = d.m, d.n, d.k, _DTYPES[d.type]
+    ld = _ld(k)
+    wp, wn, px, pw, psw, pb, py, pxq, psx, pxqt = _here(
+        workspace, (x, t, (m, k), "x"), (wq, torch.int8, (n, ld), "wq"), (sw, torch.float32, (n,), "sw"),
+        (bias, torch.float32, (n,), "bias"), (y, t, (m, n), "y"), (xq, torch.int8, (m, ld), "xq"),
+        (sx, torch.float32, (m,), "sx"), (xqt, torch.int8, (k, _ld(m)), "xqt"))
+    _check("dfp_linear_i8_fwd", lib().dfp_linear_i8_fwd(d, px, pw, psw, pb, py, pxq, psx, pxqt, wp, wn,
                                                         _stream(stream)))
 
 
 def dfp_linear_i8_bwd_data(d: LinearDesc, dy, wqt, sw, dx, workspace=None, stream=None):
-    t = _DTYPES[d.type]
-    _need_here(_here(workspace), (dy, t, (d.m, d.n), "dy"), (wqt, torch.int8, (d.k, i8_ld(d.n)), "wqt"),
-               (sw, torch.float32, (d.n,), "sw"), (dx, t, (d.m, d.k), "dx"))
-    wp, wn = _ws(workspace)
-    _check("dfp_linear_i8_bwd_data", lib().dfp_linear_i8_bwd_data(ctypes.byref(d), _ptr(dy), _ptr(wqt), _ptr(sw),
-                                                                  _ptr(dx), wp, wn, _stream(stream)))
+    m, n, k, t = d.m, d.n, d.k, _DTYPES[d.type]
+    wp, wn, pdy, pw, psw, pdx = _here(
+        workspace, (dy, t, (m, n), "dy"), (wqt, torch.int8, (k, _ld(n)), "wqt"), (sw, torch.float32, (n,), "sw"),
+        (dx, t, (m, k), "dx"))
+    _check("dfp_linear_i8_bwd_data", lib().dfp_linear_i8_bwd_data(d, pdy, pw, psw, pdx, wp, wn, _stream(stream)))
 
 
 def dfp_linear_i8_bwd_weights(d: LinearDesc, dy, xqt, sx, dw, db=None, workspace=None, stream=None):
-    _need_here(_here(workspace), (dy, _DTYPES[d.type], (d.m, d.n), "dy"),
-               (xqt, torch.int8, (d.k, i8_ld(d.m)), "xqt"), (sx, torch.float32, (d.m,), "sx"),
-               (dw, torch.float32, (d.n, d.k), "dw"), (db, torch.float32, (d.n,), "db"))
-    wp, wn = _ws(workspace)
-    _check("dfp_linear_i8_bwd_weights",
-           lib().dfp_linear_i8_bwd_weights(ctypes.byref(d), _ptr(dy), _ptr(xqt), _ptr(sx), _ptr(dw), _ptr(db), wp, wn,
-                                           _stream(stream)))
+    m, n, k = d.m, d.n, d.k
+    wp, wn, pdy, px, psx, pdw, pdb = _here(
+        workspace, (dy, _DTYPES[d.type], (m, n), "dy"), (xqt, torch.int8, (k, _ld(m)), "xqt"),
+        (sx, torch.float32, (m,), "sx"), (dw, torch.float32, (n, k), "dw"), (db, torch.float32, (n,), "db"))
+    _check("dfp_linear_i8_bwd_weights", lib().dfp_linear_i8_bwd_weights(d, pdy, px, psx, pdw, pdb, wp, wn,
+                                                                        _stream(stream)))
 
 
 def make_ortho_desc(batch, rows, cols, dtype=torch.bfloat16, steps=5, eps=1e-7,
@@ -538,10 +545,8 @@ def dfp_orthogonalize(d: OrthoDesc, x, out, workspace=None, stream=None):
     t, shapes = _DTYPES[d.type], _ortho_shapes(d)
     if x.shape not in shapes:
         raise ValueError("x must have shape %s, not %s" % (shapes[0], tuple(x.shape)))
-    _need_here(_here(workspace), (x, t, x.shape, "x"), (out, t, x.shape, "out"))
-    wp, wn = _ws(workspace)
-    _check("dfp_orthogonalize", lib().dfp_orthogonalize(ctypes.byref(d), _ptr(x), _ptr(out), wp, wn,
-                                                        _stream(stream)))
+    wp, wn, px, po = _here(workspace, (x, t, x.shape, "x"), (out, t, x.shape, "out"))
+    _check("dfp_orthogonalize", lib().dfp_orthogonalize(d, px, po, wp, wn, _stream(stream)))
 
 
 def dfp_muon_quantize(d: OrthoDesc, lr, mu, wd, scale, w, v, dw, wq=None, sw=None, wqt=None, nesterov=True,
@@ -551,13 +556,12 @@ def dfp_muon_quantize(d: OrthoDesc, lr, mu, wd, scale, w, v, dw, wq=None, sw=Non
     shapes, n = _ortho_shapes(d), d.batch * d.rows
     if w.shape not in shapes:
         raise ValueError("w must have shape %s, not %s" % (shapes[0], tuple(w.shape)))
-    _need_here(_here(workspace), (w, torch.float32, w.shape, "w"), (v, torch.float32, w.shape, "v"),
-               (dw, _DTYPES[d.type], w.shape, "dw"), (wq, torch.int8, (n, i8_ld(d.cols)), "wq"),
-               (sw, torch.float32, (n,), "sw"), (wqt, torch.int8, (d.cols, i8_ld(d.rows)), "wqt"))
-    wp, wn = _ws(workspace)
-    _check("dfp_muon_quantize", lib().dfp_muon_quantize(ctypes.byref(d), lr, mu, wd, scale, int(bool(nesterov)),
-                                                        _ptr(w), _ptr(v), _ptr(dw), _ptr(wq), _ptr(sw), _ptr(wqt), wp,
-                                                        wn, _stream(stream)))
+    wp, wn, pw, pv, pdw, pq, ps, pqt = _here(
+        workspace, (w, torch.float32, w.shape, "w"), (v, torch.float32, w.shape, "v"),
+        (dw, _DTYPES[d.type], w.shape, "dw"), (wq, torch.int8, (n, _ld(d.cols)), "wq"),
+        (sw, torch.float32, (n,), "sw"), (wqt, torch.int8, (d.cols, _ld(d.rows)), "wqt"))
+    _check("dfp_muon_quantize", lib().dfp_muon_quantize(d, lr, mu, wd, scale, int(bool(nesterov)), pw, pv, pdw, pq, ps,
+                                                        pqt, wp, wn, _stream(stream)))
 
 
 def alloc_workspace(d: Desc, direction: int, device="cuda"):
