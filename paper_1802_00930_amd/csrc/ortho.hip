@@ -2,13 +2,16 @@
 //   A = X X^T, B = b A + c A A, X = a X + B X
 // with the smaller side first (X^T X and X B where rows > cols).
 //
-// X [R][C] lives in FP32 in the caller's orientation.  The products read f16
-// operands in the layout of mma_tile.h: `gram` is X (or X^T where R > C) with its
-// longer side contiguous, `step` the other of the two; both are written by the
-// kernel that makes X.  All sides are padded to 128 with zeros, which every step
-// keeps zero.  A and B are symmetric: only tiles on and above the diagonal are
-// computed and each is stored twice.  B's diagonal, the largest entries of its
-// rows, stays out of the f16 operand and joins in FP32: X = (a + B_ii) X + B' X.
+// The products read f16 operands in the layout of mma_tile.h: `gram` is X (or X^T
+// where R > C) with its longer side contiguous, `step` the other of the two; both
+// are written by the kernel that makes X.  BF16 results: operands of one f16 number,
+// X itself beside them in FP32, [R][C].  Otherwise: operands of a high and a low f16
+// part, and X is their sum (2^-24 of a value).  All sides are padded to 64 with
+// zeros, which every step keeps zero.
+//
+// A and B are symmetric: only tiles on and above the diagonal are computed and each
+// is stored twice.  B's diagonal, the largest entries of its rows, stays out of the
+// f16 operand and joins in FP32: X = (a + B_ii) X + B' X.
 //
 // Units: X in 2^-12, A in 2^-10, B in 2^-sb so that |b A + c A A| <= 32768 in it
 // for singular values up to sqrt(2).
@@ -29,14 +32,54 @@ namespace {
 
 constexpr int kBlock = 256;
 constexpr int kUnitX = 12, kUnitA = 10;
-constexpr int kNormParts = 256;
+constexpr int kNormParts = 1024;  // most partial sums of a matrix
+
+// A product's tiles and slices by an estimate of its time (us): a piece of a tile
+// takes `alone` if a CU has one tile and `busy` a tile if it has several (512 x 512 x
+// 8192 bytes and 8192^2 outputs; one f16 number, two).  Slices mean that their sums
+// are written and read (5 TB/s) and a second kernel (4).
+struct MmPlan {
+  int32_t side, slices, per;
+  int64_t bytes;
+};
+struct TileKind {
+  int32_t side;
+  double alone[2], busy[2];
+};
+constexpr TileKind kKinds[] = {{256, {1.38, 1.74}, {1.74, 2.21}}, {128, {0.57, 0.64}, {0.58, 0.61}},
+                               {64, {0.29, 0.32}, {0.18, 0.20}}};
+constexpr int64_t kMostPartBytes = 128 << 20;
+
+MmPlan plan_mm(int64_t m, int64_t n, int64_t pieces, int64_t batch, bool symmetric, bool sliceable, bool split) {
+  MmPlan best{};
+  double least = 1e30;
+  for (const TileKind& kind : kKinds) {
+    const int64_t tm = (m + kind.side - 1) / kind.side, tn = (n + kind.side - 1) / kind.side;
+    const int64_t tiles = (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batch;
+    for (int64_t s = 1; s <= (sliceable ? 32 : 1) && s <= pieces; ++s) {
+      const int64_t per = (pieces + s - 1) / s, used = (pieces + per - 1) / per;
+      if (used != s) continue;
+      const int64_t bytes = s > 1 ? s * tiles * kind.side * kind.side * 4 : 0;
+      if (bytes > kMostPartBytes) break;
+      const int64_t a_cu = (tiles * s + 255) / 256;
+      double us = per * std::max(kind.alone[split], a_cu * kind.busy[split]);
+      if (s > 1) us += 4. + 2. * bytes / 5e6;
+      if (us < least) {
+        least = us;
+        best = {kind.side, (int32_t)s, (int32_t)per, bytes};
+      }
+    }
+  }
+  return best;
+}
 
 struct Plan {
   bool tall;             // rows > cols
   int64_t R, C, Rp, Cp;  // the matrix, padded
   int64_t r, rp;         // the smaller side, padded
   int64_t e;             // bytes of an operand element
-  int64_t x32, gram, step0, step1, aa, bb, diag, norm, bytes;  // offsets, total
+  int64_t x32, gram, step0, step1, aa, bb, diag, norm, slices, bytes;  // offsets, total
+  MmPlan mgram, mpoly, mstep;
 };
 
 Plan make_plan(const dfp_ortho_desc& d, bool split) {
@@ -44,8 +87,8 @@ Plan make_plan(const dfp_ortho_desc& d, bool split) {
   p.R = d.rows;
   p.C = d.cols;
   p.tall = d.rows > d.cols;
-  p.Rp = (p.R + 127) / 128 * 128;
-  p.Cp = (p.C + 127) / 128 * 128;
+  p.Rp = (p.R + 63) / 64 * 64;
+  p.Cp = (p.C + 63) / 64 * 64;
   p.r = p.tall ? p.C : p.R;
   p.rp = p.tall ? p.Cp : p.Rp;
   p.e = split ? 4 : 2;
@@ -56,7 +99,11 @@ Plan make_plan(const dfp_ortho_desc& d, bool split) {
     return o;
   };
   const int64_t n = p.Rp * p.Cp * d.batch, s = p.rp * p.rp * d.batch;
-  p.x32 = take(n * 4);
+  const int64_t per_piece = split ? 32 : 64;
+  p.mgram = plan_mm(p.rp, p.rp, (p.tall ? p.Rp : p.Cp) / per_piece, d.batch, true, true, split);
+  p.mpoly = plan_mm(p.rp, p.rp, p.rp / per_piece, d.batch, true, true, split);
+  p.mstep = plan_mm(p.Rp, p.Cp, p.rp / per_piece, d.batch, false, false, split);
+  p.x32 = take(split ? 0 : n * 4);
   p.gram = take(n * p.e);
   p.step0 = take(n * p.e);
   p.step1 = take(n * p.e);
@@ -64,11 +111,10 @@ Plan make_plan(const dfp_ortho_desc& d, bool split) {
   p.bb = take(s * p.e);
   p.diag = take(p.rp * d.batch * 4);
   p.norm = take((int64_t)kNormParts * d.batch * 8);
+  p.slices = take(std::max(p.mgram.bytes, p.mpoly.bytes));
   p.bytes = at;
   return p;
 }
-
-bool splits(int32_t type) { return type != DFP_BF16; }
 
 // ---------------------------------------------------------------- operands
 // Byte offset of element k of a row.
@@ -79,15 +125,8 @@ __device__ __forceinline__ int64_t op_off(int64_t k) {
 __device__ __forceinline__ uint16_t h_bits(_Float16 h) { return __builtin_bit_cast(uint16_t, h); }
 __device__ __forceinline__ float h_val(uint32_t b) { return (float)__builtin_bit_cast(_Float16, (uint16_t)b); }
 
-// v (in units already) to element k of the row at p.
-template <Prod P>
-__device__ __forceinline__ void put1(uint8_t* p, int64_t k, float v) {
-  uint16_t* d = (uint16_t*)(p + op_off<P>(k));
-  const _Float16 hi = (_Float16)v;
-  d[0] = h_bits(hi);
-  if (P == Prod::F16X2) d[32] = h_bits((_Float16)(v - (float)hi));
-}
-// Four elements k .. k + 3, k a multiple of 4.
+// v (in units already) to elements of the row at p: four k .. k + 3, k a multiple of 4,
+// or eight.
 template <Prod P>
 __device__ __forceinline__ void put4(uint8_t* p, int64_t k, const float (&v)[4]) {
   uint32_t hi[4], lo[4];
@@ -148,78 +187,96 @@ __device__ __forceinline__ void direction(const Source<T>& s, int64_t at, int64_
   }
 }
 
-// Momentum update and partial sums of u^2 (in 64 bits), kNormParts a matrix.
+// Momentum update and partial sums of u^2 (in 64 bits), gridDim.x a matrix.
 template <int T, bool MUON>
 __global__ __launch_bounds__(kBlock) void k_norm(Source<T> s, int64_t n, double* __restrict__ part) {
   __shared__ double red[kBlock / 64];
-  const int64_t base = (int64_t)blockIdx.y * n;
+  const int64_t base = (int64_t)blockIdx.y * n, stride = (int64_t)gridDim.x * kBlock * 4;
   double sum = 0.;
-  for (int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) * 4; i < n; i += (int64_t)kNormParts * kBlock * 4) {
-    float u[4];
-    if (MUON) {
-      float g[4], v[4];
-      load_n<T, 4>(s.x + base + i, n - i, g);
-      load_n<DFP_F32, 4>(s.v + base + i, n - i, v);
+  constexpr int U = 4;  // quads in flight
+  for (int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) * 4; i < n; i += stride * U) {
+    float g[U][4], v[U][4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        v[j] = fmaf(s.mu, v[j], g[j]);
-        u[j] = s.nesterov ? fmaf(s.mu, v[j], g[j]) : v[j];
-      }
-      store_n<DFP_F32, 4>(s.v + base + i, n - i, v);
-    } else {
-      load_n<T, 4>(s.x + base + i, n - i, u);
+    for (int k = 0; k < U; ++k) {
+      const int64_t at = i + k * stride;
+      load_n<T, 4>(s.x + base + at, n - at, g[k]);
+      if (MUON) load_n<DFP_F32, 4>(s.v + base + at, n - at, v[k]);
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sum += (double)u[j] * (double)u[j];
+    for (int k = 0; k < U; ++k) {
+      const int64_t at = i + k * stride;
+      if (MUON) {
+        float u[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          v[k][j] = fmaf(s.mu, v[k][j], g[k][j]);
+          u[j] = s.nesterov ? fmaf(s.mu, v[k][j], g[k][j]) : v[k][j];
+          sum += (double)u[j] * (double)u[j];
+        }
+        store_n<DFP_F32, 4>(s.v + base + at, n - at, v[k]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum += (double)g[k][j] * (double)g[k][j];
+      }
+    }
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = sum;
   __syncthreads();
-  if (threadIdx.x == 0) part[(int64_t)blockIdx.y * kNormParts + blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
+  if (threadIdx.x == 0)
+    part[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// X = u / (|u| + eps): FP32 and both operands, 64 x 64 tiles of the padded matrix.
+// X = u / (|u| + eps): both operands (and FP32), 64 x 64 tiles of the padded matrix.
 template <int T, bool MUON, Prod P>
 __global__ __launch_bounds__(kBlock) void k_pack(Source<T> s, int64_t R, int64_t C, int64_t Rp, int64_t Cp,
-                                                 const double* __restrict__ part, float eps, float* __restrict__ x32,
-                                                 uint8_t* __restrict__ rowop, uint8_t* __restrict__ colop) {
+                                                 const double* __restrict__ part, int32_t parts, float eps,
+                                                 float* __restrict__ x32, uint8_t* __restrict__ rowop,
+                                                 uint8_t* __restrict__ colop) {
   __shared__ float tile[64][65];
   __shared__ double red[kBlock / 64];
   const int64_t b = blockIdx.y;
-  double sum = part[b * kNormParts + threadIdx.x];
+  const int64_t ct = Cp / 64, r0 = blockIdx.x / ct * 64, c0 = blockIdx.x % ct * 64;
+  const int cc = (threadIdx.x & 15) * 4;
+  float u[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t r = r0 + (threadIdx.x >> 4) + i * 16, c = c0 + cc;
+    u[i][0] = u[i][1] = u[i][2] = u[i][3] = 0.f;
+    if (r < R && c < C) direction<T, MUON>(s, (b * R + r) * C + c, C - c, u[i]);
+  }
+  double sum = 0.;
+  for (int32_t i = threadIdx.x; i < parts; i += kBlock) sum += part[b * parts + i];
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = sum;
   __syncthreads();
   const double nrm = sqrt((red[0] + red[1]) + (red[2] + red[3]));
   const double inv = isfinite(nrm) ? 1. / (nrm + (double)eps) : (double)__uint_as_float(0x7fc00000u);
-  const int64_t ct = Cp / 64, r0 = blockIdx.x / ct * 64, c0 = blockIdx.x % ct * 64;
-  const int cc = (threadIdx.x & 15) * 4;
-  const int64_t pbytes = Rp * Cp * (P == Prod::F16X2 ? 4 : 2);
   constexpr int64_t e = P == Prod::F16X2 ? 4 : 2;
+  const int64_t pbytes = Rp * Cp * e;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int rr = (threadIdx.x >> 4) + i * 16;
     const int64_t r = r0 + rr, c = c0 + cc;
-    float u[4] = {0.f, 0.f, 0.f, 0.f};
-    if (r < R && c < C) direction<T, MUON>(s, (b * R + r) * C + c, C - c, u);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) u[j] = r < R && c + j < C ? (float)((double)u[j] * inv) : 0.f;
-    *(float4*)(x32 + (b * Rp + r) * Cp + c) = make_float4(u[0], u[1], u[2], u[3]);
+    for (int j = 0; j < 4; ++j) u[i][j] = r < R && c + j < C ? (float)((double)u[i][j] * inv) : 0.f;
+    if (P == Prod::F16)
+      *(float4*)(x32 + (b * Rp + r) * Cp + c) = make_float4(u[i][0], u[i][1], u[i][2], u[i][3]);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      u[j] *= (float)(1 << kUnitX);
-      tile[rr][cc + j] = u[j];
+      u[i][j] *= (float)(1 << kUnitX);
+      tile[rr][cc + j] = u[i][j];
     }
-    put4<P>(rowop + b * pbytes + r * Cp * e, c, u);
+    put4<P>(rowop + b * pbytes + r * Cp * e, c, u[i]);
   }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int rr = (threadIdx.x >> 4) + i * 16;
-    const float u[4] = {tile[cc][rr], tile[cc + 1][rr], tile[cc + 2][rr], tile[cc + 3][rr]};
-    put4<P>(colop + b * pbytes + (c0 + rr) * Rp * e, r0 + cc, u);
+    const float v[4] = {tile[cc][rr], tile[cc + 1][rr], tile[cc + 2][rr], tile[cc + 3][rr]};
+    put4<P>(colop + b * pbytes + (c0 + rr) * Rp * e, r0 + cc, v);
   }
 }
 
@@ -229,17 +286,19 @@ struct MmArgs {
   int64_t lda, ldb;        // bytes of a row
   int64_t sa, sb;          // bytes of a matrix
   int32_t m, n;            // padded sides of the output
-  int32_t pieces;
+  int32_t pieces, per;     // of the reduction, of a slice
+  int32_t slices;
   uint32_t tm, tn;
+  float* part;             // slices: [batch][tile][slice][quad][thread] of four sums
   float unit;              // of the sum
   // outputs
   uint8_t *rowop, *colop;  // operand and (GRAM / POLY: the same) its transpose
   int64_t ldr, ldc, sr, sc;
-  const uint8_t* aa;       // POLY: A
+  const uint8_t* old;      // POLY: A; STEP, LAST of two parts: X, in rowop's layout
   float* diag;             // POLY writes, STEP reads, [rp] a matrix
   float cb, cc, ca;        // coefficients
   float uout;              // unit of the operands written
-  float* x32;
+  float* x32;              // one part: X
   int32_t R, C, rp;
   bool diag_cols;          // the diagonal goes by column (tall)
   void* out;
@@ -261,76 +320,194 @@ __device__ __forceinline__ void tri_tile(uint32_t id, uint32_t t, uint32_t* i, u
   *j = row + id;
 }
 
-template <Prod P, int KIND, int T, bool MUON, int TM, int TN, int WM, int WN, int S>
+template <int KIND>
+__device__ __forceinline__ void mm_tile(const MmArgs& g, uint32_t id, uint32_t* im, uint32_t* in) {
+  if (KIND == GRAM || KIND == POLY)
+    tri_tile(id, g.tm, im, in);
+  else
+    tile_of(id, g.tm, g.tn, 8, im, in);
+}
+
+// What becomes of a wave's sums at 16 FM rows from i0 by 32 columns from j0 (a lane:
+// rows i0 + 16 fi + lane % 16, columns j0 + 8 (lane / 16) ..).  The transposed operand
+// goes through LDS (`lds`: 32 columns of 16 FM + 8 numbers, this wave's own) so that it
+// is stored in 16-byte runs too: stored from the lanes, two bytes at a time,
+// 2048 x 8192's STEP took 217 us.
+template <Prod P, int KIND, int T, bool MUON, int FM>
+__device__ __forceinline__ void finish(const MmArgs& g, int64_t b, int64_t i0, int64_t j0, bool mirror, uint16_t* lds,
+                                       float (&s)[FM][8]) {
+  constexpr int kRows = 16 * FM, kStride = kRows + 8;
+  const int lane = threadIdx.x & 63;
+  const int64_t j = j0 + (lane >> 4) * 8;
+  const bool in_n = j < g.n;
+#pragma unroll
+  for (int fi = 0; fi < FM; ++fi) {
+    const int64_t i = i0 + fi * 16 + (lane & 15);
+    float(&v)[8] = s[fi];
+    if (i >= g.m || !in_n) continue;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) v[r] *= g.unit;
+    if (KIND == POLY) {
+      float a[8];
+      get8<P>(g.old + b * g.sr + i * g.ldr, j, a);
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        v[r] = fmaf(g.cc, v[r], g.cb * (a[r] * (1.f / (1 << kUnitA))));
+        if (i == j + r) {
+          g.diag[b * g.rp + i] = v[r];
+          v[r] = 0.f;
+        }
+      }
+    }
+    if (KIND == STEP || KIND == LAST) {
+      float x[8];
+      float* px = g.x32 + (b * g.m + i) * (int64_t)g.n + j;
+      if (P == Prod::F16) {
+        load_n<DFP_F32, 8>(px, x);
+      } else {
+        get8<P>(g.old + b * g.sr + i * g.ldr, j, x);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) x[r] *= 1.f / (1 << kUnitX);
+      }
+#pragma unroll
+      for (int r = 0; r < 8; ++r) v[r] = fmaf(g.ca + g.diag[b * g.rp + (g.diag_cols ? j + r : i)], x[r], v[r]);
+      if (KIND == STEP && P == Prod::F16) store_n<DFP_F32, 8>(px, v);
+    }
+    if (KIND == LAST) {
+      if (i >= g.R || j >= g.C) continue;
+      const int64_t at = (b * g.R + i) * g.C + j;
+      if (MUON) {
+        float w[8];
+        load_n<DFP_F32, 8>(g.w + at, g.C - j, w);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) w[r] = fmaf(-g.alpha, v[r], g.keep * w[r]);
+        store_n<DFP_F32, 8>(g.w + at, g.C - j, w);
+      } else {
+        store_n<T, 8>((typename Elem<T>::type*)g.out + at, g.C - j, v);
+      }
+      continue;
+    }
+#pragma unroll
+    for (int r = 0; r < 8; ++r) v[r] *= g.uout;
+    put8<P>(g.rowop + b * g.sr + i * g.ldr, j, v);
+  }
+  if (KIND == LAST || !mirror) return;
+  // (g.m is a multiple of 64: a wave's rows are all in or, from kRows = 64 on, all out)
+#pragma unroll
+  for (int part = 0; part < (P == Prod::F16X2 ? 2 : 1); ++part) {
+#pragma unroll
+    for (int fi = 0; fi < FM; ++fi)
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        const _Float16 hi = (_Float16)s[fi][r];
+        lds[((lane >> 4) * 8 + r) * kStride + fi * 16 + (lane & 15)] =
+            h_bits(part ? (_Float16)(s[fi][r] - (float)hi) : hi);
+      }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int k = 0; k < kRows / 16; ++k) {
+      const int c = k * (512 / kRows) + lane / (kRows / 8), q = lane % (kRows / 8) * 8;
+      const uint4 d = *(const uint4*)(lds + c * kStride + q);
+      if (j0 + c < g.n && i0 + q < g.m)
+        *(uint4*)(g.colop + b * g.sc + (j0 + c) * g.ldc + op_off<P>(i0 + q) + part * 64) = d;
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+template <Prod P, int KIND, int T, bool MUON, bool SLICED, int TM, int TN, int WM, int WN, int S>
 __global__ __launch_bounds__(64 * WM * WN, 2) void k_mm(MmArgs g) {
   typedef MmaTile<P, TM, TN, WM, WN, S> Tile;
   const int64_t b = blockIdx.y;
   uint32_t im, in;
-  if (KIND == GRAM || KIND == POLY)
-    tri_tile(blockIdx.x, g.tm, &im, &in);
-  else
-    tile_of(blockIdx.x, g.tm, g.tn, 8, &im, &in);
-  const int64_t i0 = (int64_t)im * TM, j0 = (int64_t)in * TN;
+  mm_tile<KIND>(g, SLICED ? blockIdx.x / g.slices : blockIdx.x, &im, &in);
+  const int32_t slice = SLICED ? blockIdx.x % g.slices : 0;
+  const int32_t p0 = slice * g.per, pieces = SLICED ? min(g.per, g.pieces - p0) : g.pieces;
+  const int64_t i0 = (int64_t)im * TM, j0 = (int64_t)in * TN, at = (int64_t)p0 * kPiece;
   mv4f acc[Tile::FM][Tile::FN];
-  Tile::run(g.a + b * g.sa + i0 * g.lda, g.lda, (int32_t)(g.m - i0), g.b + b * g.sb + j0 * g.ldb, g.ldb,
-            (int32_t)(g.n - j0), g.pieces, acc);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t i1 = i0 + (wave / WN) * (TM / WM) + (lane & 15);
-  const int64_t j1 = j0 + (wave % WN) * (TN / WN) + (lane >> 4) * 8;
+  Tile::run(g.a + b * g.sa + i0 * g.lda + at, g.lda, (int32_t)(g.m - i0), g.b + b * g.sb + j0 * g.ldb + at, g.ldb,
+            (int32_t)(g.n - j0), pieces, acc);
+  if (SLICED) {
+    mv4f* d = (mv4f*)g.part + (b * gridDim.x + blockIdx.x) * (int64_t)(TM * TN / 4) + threadIdx.x;
 #pragma unroll
-  for (int fj = 0; fj < Tile::FN; fj += 2)
+    for (int j = 0; j < Tile::FN; ++j)
 #pragma unroll
-    for (int fi = 0; fi < Tile::FM; ++fi) {
-      const int64_t i = i1 + fi * 16, j = j1 + fj * 16;
-      if (i >= g.m || j >= g.n) continue;
-      float v[8];
+      for (int i = 0; i < Tile::FM; ++i) d[(j * Tile::FM + i) * Tile::kThreads] = acc[i][j];
+    return;
+  }
+  const int wave = threadIdx.x >> 6;
+  __syncthreads();  // all waves are done with the stages
+  uint16_t* lds = (uint16_t*)(Tile::template stage<0>() + wave * (Tile::kStage / (WM * WN)));
+  static_assert(32 * (16 * Tile::FM + 8) * 2 <= Tile::kStage / (WM * WN), "a wave's part of a stage");
 #pragma unroll
-      for (int r = 0; r < 8; ++r) v[r] = acc[fi][fj + (r >> 2)][r & 3] * g.unit;
-      if (KIND == POLY) {
-        float a[8];
-        get8<P>(g.aa + b * g.sr + i * g.ldr, j, a);
+  for (int j = 0; j < Tile::FN; j += 2) {
+    float s[Tile::FM][8];
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-          v[r] = fmaf(g.cc, v[r], g.cb * (a[r] * (1.f / (1 << kUnitA))));
-          if (i == j + r) {
-            g.diag[b * g.rp + i] = v[r];
-            v[r] = 0.f;
-          }
-        }
-      }
-      if (KIND == STEP || KIND == LAST) {
-        float* px = g.x32 + (b * g.m + i) * (int64_t)g.n + j;
-        const float4 x0 = *(const float4*)px, x1 = *(const float4*)(px + 4);
-        const float xs[8] = {x0.x, x0.y, x0.z, x0.w, x1.x, x1.y, x1.z, x1.w};
+    for (int i = 0; i < Tile::FM; ++i)
 #pragma unroll
-        for (int r = 0; r < 8; ++r) v[r] = fmaf(g.ca + g.diag[b * g.rp + (g.diag_cols ? j + r : i)], xs[r], v[r]);
-        if (KIND == STEP) {
-          *(float4*)px = make_float4(v[0], v[1], v[2], v[3]);
-          *(float4*)(px + 4) = make_float4(v[4], v[5], v[6], v[7]);
-        }
-      }
-      if (KIND == LAST) {
-        if (i >= g.R || j >= g.C) continue;
-        const int64_t at = (b * g.R + i) * g.C + j;
-        if (MUON) {
-          float w[8];
-          load_n<DFP_F32, 8>(g.w + at, g.C - j, w);
+      for (int r = 0; r < 8; ++r) s[i][r] = acc[i][j + (r >> 2)][r & 3];
+    finish<P, KIND, T, MUON, Tile::FM>(g, b, i0 + (wave / WN) * (TM / WM), j0 + (wave % WN) * (TN / WN) + j * 16,
+                                       KIND == STEP || im != in, lds, s);
+  }
+}
+
+// The slices of a tile added up in their order, then as above: workgroups of a tile's
+// threads by one pair of fragment columns.
+template <Prod P, int KIND, int TM, int TN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void k_sum(MmArgs g) {
+  typedef MmaTile<P, TM, TN, WM, WN, 2> Tile;
+  constexpr int FM = Tile::FM, FN = Tile::FN;
+  __shared__ __align__(16) uint16_t lds[WM * WN][32 * (16 * FM + 8)];
+  const int64_t b = blockIdx.y;
+  const uint32_t id = blockIdx.x / (FN / 2), j = blockIdx.x % (FN / 2) * 2;
+  uint32_t im, in;
+  mm_tile<KIND>(g, id, &im, &in);
+  const int64_t tiles = gridDim.x / (FN / 2);
+  const mv4f* d = (const mv4f*)g.part + (b * tiles + id) * g.slices * (int64_t)(TM * TN / 4) + threadIdx.x;
+  float s[FM][8] = {};
+  for (int32_t k = 0; k < g.slices; ++k, d += TM * TN / 4) {
+    mv4f v[FM][2];
 #pragma unroll
-          for (int r = 0; r < 8; ++r) w[r] = fmaf(-g.alpha, v[r], g.keep * w[r]);
-          store_n<DFP_F32, 8>(g.w + at, g.C - j, w);
-        } else {
-          store_n<T, 8>((typename Elem<T>::type*)g.out + at, g.C - j, v);
-        }
-        continue;
-      }
+    for (int i = 0; i < FM; ++i)
 #pragma unroll
-      for (int r = 0; r < 8; ++r) v[r] *= g.uout;
-      put8<P>(g.rowop + b * g.sr + i * g.ldr, j, v);
-      if (KIND == STEP || im != in) {
+      for (int h = 0; h < 2; ++h) v[i][h] = d[((j + h) * FM + i) * Tile::kThreads];
 #pragma unroll
-        for (int r = 0; r < 8; ++r) put1<P>(g.colop + b * g.sc + (j + r) * g.ldc, i, v[r]);
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int r = 0; r < 8; ++r) s[i][r] += v[i][r >> 2][r & 3];
+  }
+  const int wave = threadIdx.x >> 6;
+  finish<P, KIND, 0, false, FM>(g, b, (int64_t)im * TM + (wave / WN) * (TM / WM),
+                                (int64_t)in * TN + (wave % WN) * (TN / WN) + j * 16, im != in, lds[wave], s);
+}
+
+template <Prod P, int KIND, int T, bool MUON>
+dfp_status launch_mm(int32_t id, const MmPlan& p, int32_t batch, MmArgs& g, hipStream_t st) {
+  g.tm = (uint32_t)((g.m + p.side - 1) / p.side);
+  g.tn = (uint32_t)((g.n + p.side - 1) / p.side);
+  g.per = p.per;
+  g.slices = p.slices;
+  constexpr bool SYM = KIND == GRAM || KIND == POLY;
+  const uint32_t tiles = SYM ? g.tm * (g.tm + 1) / 2 : g.tm * g.tn;
+  auto go = [&](auto side, auto wm, auto wn, auto s) -> dfp_status {
+    constexpr int D = decltype(side)::value, WM = decltype(wm)::value, WN = decltype(wn)::value;
+    constexpr int S = decltype(s)::value;
+    const dim3 block(64 * WM * WN);
+    if constexpr (SYM) {
+      if (p.slices > 1) {
+        DFP_LAUNCH(id, (k_mm<P, KIND, T, MUON, true, D, D, WM, WN, S>), dim3(tiles * p.slices, (unsigned)batch), block,
+                   0, st, g);
+        DFP_LAUNCH(id, (k_sum<P, KIND, D, D, WM, WN>), dim3(tiles * (D / WN / 32), (unsigned)batch), block, 0, st, g);
+        return DFP_OK;
       }
     }
+    DFP_LAUNCH(id, (k_mm<P, KIND, T, MUON, false, D, D, WM, WN, S>), dim3(tiles, (unsigned)batch), block, 0, st, g);
+    return DFP_OK;
+  };
+  typedef std::integral_constant<int, 2> Two;
+  if (p.side == 256) return go(std::integral_constant<int, 256>(), std::integral_constant<int, 4>(), Two(), Two());
+  if (p.side == 128) return go(std::integral_constant<int, 128>(), Two(), Two(), Two());
+  return go(std::integral_constant<int, 64>(), Two(), Two(), std::integral_constant<int, 3>());
 }
 
 // Largest unit of B that keeps |b A + c A A| at 32768 or less for |X| <= sqrt(2).
@@ -353,22 +530,24 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
   uint8_t* step[2] = {base + p.step0, base + p.step1};
   double* part = (double*)(base + p.norm);
   const unsigned nb = (unsigned)d.batch;
-  DFP_LAUNCH(K_ORTHO_NORM, (k_norm<T, MUON>), dim3(kNormParts, nb), dim3(kBlock), 0, st, src, p.R * p.C, part);
+  const int64_t n = p.R * p.C;
+  const int32_t parts = (int32_t)std::min<int64_t>(kNormParts, (n + kBlock * 4 - 1) / (kBlock * 4));
+  DFP_LAUNCH(K_ORTHO_NORM, (k_norm<T, MUON>), dim3((unsigned)parts, nb), dim3(kBlock), 0, st, src, n, part);
   // gram: the longer side contiguous
   uint8_t* rowop = p.tall ? step[0] : gram;
   uint8_t* colop = p.tall ? gram : step[0];
   DFP_LAUNCH(K_ORTHO_PACK, (k_pack<T, MUON, P>), dim3((unsigned)(p.Rp / 64 * (p.Cp / 64)), nb), dim3(kBlock), 0, st,
-             src, p.R, p.C, p.Rp, p.Cp, part, d.eps, x32, rowop, colop);
+             src, p.R, p.C, p.Rp, p.Cp, part, parts, d.eps, x32, rowop, colop);
   const int64_t longer = p.tall ? p.Rp : p.Cp;
   const int64_t sx = p.Rp * p.Cp * p.e, ss = p.rp * p.rp * p.e;
   constexpr float kInvX = 1.f / (1 << kUnitX), kInvA = 1.f / (1 << kUnitA);
-  constexpr int TM = 128, TN = 128;
   for (int32_t s = 0; s < d.steps; ++s) {
     const float ub = unit_b(d.coef[s]);
-    const uint32_t ts = (uint32_t)(p.rp / TM);
+    dfp_status rc;
     MmArgs g{};
     g.rp = (int32_t)p.rp;
     g.diag = (float*)(base + p.diag);
+    g.part = (float*)(base + p.slices);
     g.ca = d.coef[s][0], g.cb = d.coef[s][1], g.cc = d.coef[s][2];
     // A = X X^T
     g.a = g.b = gram;
@@ -376,22 +555,21 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
     g.sa = g.sb = sx;
     g.m = g.n = (int32_t)p.rp;
     g.pieces = (int32_t)(longer / kPerPiece);
-    g.tm = g.tn = ts;
     g.unit = kInvX * kInvX;
     g.uout = (float)(1 << kUnitA);
     g.rowop = g.colop = aa;
     g.ldr = g.ldc = p.rp * p.e;
     g.sr = g.sc = ss;
-    DFP_LAUNCH(K_ORTHO_GRAM, (k_mm<P, GRAM, 0, false, TM, TN, 2, 2, 2>), dim3(ts * (ts + 1) / 2, nb), dim3(256), 0, st, g);
+    if ((rc = launch_mm<P, GRAM, 0, false>(K_ORTHO_GRAM, p.mgram, d.batch, g, st)) != DFP_OK) return rc;
     // B = b A + c A A
-    g.a = g.b = g.aa = aa;
+    g.a = g.b = g.old = aa;
     g.lda = g.ldb = p.rp * p.e;
     g.sa = g.sb = ss;
     g.pieces = (int32_t)(p.rp / kPerPiece);
     g.unit = kInvA * kInvA;
     g.uout = ub;
     g.rowop = g.colop = bb;
-    DFP_LAUNCH(K_ORTHO_POLY, (k_mm<P, POLY, 0, false, TM, TN, 2, 2, 2>), dim3(ts * (ts + 1) / 2, nb), dim3(256), 0, st, g);
+    if ((rc = launch_mm<P, POLY, 0, false>(K_ORTHO_POLY, p.mpoly, d.batch, g, st)) != DFP_OK) return rc;
     // X = a X + B X, in the caller's orientation: rows of B by rows of X^T, or rows of X by rows of B
     uint8_t *from = step[s & 1], *to = step[(s + 1) & 1];
     g.a = p.tall ? from : bb;
@@ -399,11 +577,11 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
     g.sa = p.tall ? sx : ss;
     g.sb = p.tall ? ss : sx;
     g.m = (int32_t)p.Rp, g.n = (int32_t)p.Cp;
-    g.tm = (uint32_t)(p.Rp / TM), g.tn = (uint32_t)(p.Cp / TN);
     g.unit = kInvX / ub;
     g.uout = (float)(1 << kUnitX);
     g.rowop = p.tall ? to : gram;
     g.colop = p.tall ? gram : to;
+    g.old = p.tall ? from : gram;
     g.ldr = p.Cp * p.e, g.ldc = p.Rp * p.e;
     g.sr = g.sc = sx;
     g.x32 = x32;
@@ -412,18 +590,21 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
     g.out = out;
     g.w = w;
     g.alpha = alpha, g.keep = keep;
-    const dim3 grid(g.tm * g.tn, nb);
     if (s + 1 < d.steps)
-      DFP_LAUNCH(K_ORTHO_STEP, (k_mm<P, STEP, 0, false, TM, TN, 2, 2, 2>), grid, dim3(256), 0, st, g);
+      rc = launch_mm<P, STEP, 0, false>(K_ORTHO_STEP, p.mstep, d.batch, g, st);
     else
-      DFP_LAUNCH(K_ORTHO_STEP, (k_mm<P, LAST, T, MUON, TM, TN, 2, 2, 2>), grid, dim3(256), 0, st, g);
+      rc = launch_mm<P, LAST, T, MUON>(K_ORTHO_STEP, p.mstep, d.batch, g, st);
+    if (rc != DFP_OK) return rc;
   }
   return DFP_OK;
 }
 
 }  // namespace
 
-size_t ortho_workspace_bytes(const dfp_ortho_desc& d) { return (size_t)make_plan(d, true).bytes; }
+// (either precision: one descriptor serves both calls)
+size_t ortho_workspace_bytes(const dfp_ortho_desc& d) {
+  return (size_t)std::max(make_plan(d, true).bytes, make_plan(d, false).bytes);
+}
 
 dfp_status launch_orthogonalize(const dfp_ortho_desc& d, const void* x, void* out, void* ws, hipStream_t st) {
   return with_type(d.type, [&](auto tc) -> dfp_status {
