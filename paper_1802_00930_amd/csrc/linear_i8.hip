@@ -45,14 +45,15 @@ __device__ __forceinline__ void store_quad(const I8Args& g, int64_t i, int64_t j
   store_n<T, 4>((typename Elem<T>::type*)g.out + i * g.n + j, g.n - j, v);
 }
 
-// grid.y: slices.  SLICED: the sums go to g.part instead.
+// SLICED: the tiles of every slice in turn, their sums to g.part.
 template <int T, bool SLICED, int TM, int TN, int WM, int WN, int S>
 __global__ __launch_bounds__(64 * WM * WN, 2) void k_tiles(I8Args g) {
   typedef MmaTile<Prod::I8, TM, TN, WM, WN, S> Tile;
+  const uint32_t id = xcd_order(blockIdx.x, gridDim.x), tiles = g.tm * g.tn, slice = SLICED ? id / tiles : 0;
   uint32_t im, in;
-  tile_of(blockIdx.x, g.tm, g.tn, 8, &im, &in);
+  tile_of(id - slice * tiles, g.tm, g.tn, 8, &im, &in);
   const int64_t i0 = (int64_t)im * TM, j0 = (int64_t)in * TN;
-  const int32_t p0 = SLICED ? (int32_t)blockIdx.y * g.per : 0;
+  const int32_t p0 = (int32_t)slice * g.per;
   const int32_t pieces = SLICED ? min(g.per, (int32_t)(g.ld / kPiece) - p0) : (int32_t)(g.ld / kPiece);
   mv4i acc[Tile::FM][Tile::FN];
   Tile::run(g.a + i0 * g.ld + (int64_t)p0 * kPiece, g.ld, (int32_t)(g.m - i0),
@@ -86,7 +87,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_tiles(I8Args g) {
         }
       }
       if (SLICED)
-        store_n<DFP_F32, 8>((float*)g.part + ((int64_t)blockIdx.y * g.m + ii) * g.n + jj, g.n - jj, v);
+        store_n<DFP_F32, 8>((float*)g.part + ((int64_t)slice * g.m + ii) * g.n + jj, g.n - jj, v);
       else
         store_n<T, 8>((typename Elem<T>::type*)g.out + ii * g.n + jj, g.n - jj, v);
     }
@@ -340,7 +341,7 @@ dfp_status launch_gemm_i8(int32_t m, int32_t n, int32_t k, const int8_t* a, cons
     g.tn = (uint32_t)(((int64_t)n + p.side - 1) / p.side);
     auto tiles = [&](auto sliced) -> dfp_status {
       constexpr bool SL = decltype(sliced)::value;
-      const dim3 grid(g.tm * g.tn, (unsigned)p.slices);
+      const dim3 grid(g.tm * g.tn * (unsigned)p.slices);
       // (a sliced kernel stores integers: one instance serves every type)
       constexpr int TT = SL ? DFP_F32 : T;
       if (p.side == 256)

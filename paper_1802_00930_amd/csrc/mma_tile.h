@@ -186,16 +186,41 @@ struct MmaTile {
   }
 };
 
-// Workgroup -> tile: consecutive workgroups go round the 8 XCDs, each with an L2
-// of its own.  An XCD takes a contiguous run of tiles, walked in bands of `band`
-// tile rows, so that the tiles it has in flight share rows of both operands.
-__device__ __forceinline__ void tile_of(uint32_t id, uint32_t tm, uint32_t tn, uint32_t band, uint32_t* im,
+// Consecutive workgroups go round the 8 XCDs, each with an L2 of its own: this turns
+// a workgroup's number into one that is consecutive within an XCD, so that the
+// tiles an XCD has in flight share operand rows.
+__device__ __forceinline__ uint32_t xcd_order(uint32_t id, uint32_t total) {
+  const uint32_t xcd = id & 7, q = total >> 3, rem = total & 7;
+  return xcd * q + min(xcd, rem) + (id >> 3);
+}
+// Tile t of tm x tn, walked in bands of `band` tile rows.
+__device__ __forceinline__ void tile_of(uint32_t t, uint32_t tm, uint32_t tn, uint32_t band, uint32_t* im,
                                         uint32_t* in) {
-  const uint32_t total = tm * tn, xcd = id & 7, q = total >> 3, rem = total & 7;
-  const uint32_t t = xcd * q + min(xcd, rem) + (id >> 3);
   const uint32_t per = band * tn, b = t / per, first = b * band, h = min(band, tm - first), w = t - b * per;
   *im = first + w % h;
   *in = w / h;
+}
+// Tile (i, j), i <= j, of the upper triangle of n tiles a side, in such bands.
+__device__ __forceinline__ void tri_tile_of(uint32_t t, uint32_t n, uint32_t band, uint32_t* im, uint32_t* in) {
+  uint32_t first = 0, h, corner;
+  for (;;) {
+    h = min(band, n - first);
+    corner = h * (h + 1) / 2;
+    const uint32_t count = corner + h * (n - first - h);
+    if (t < count) break;
+    t -= count;
+    first += h;
+  }
+  if (t < corner) {
+    uint32_t c = 0;
+    while (t > c) t -= ++c;  // column c of the corner has c + 1 tiles
+    *im = first + t;
+    *in = first + c;
+  } else {
+    t -= corner;
+    *im = first + t % h;
+    *in = first + h + t / h;
+  }
 }
 
 }  // namespace dfp

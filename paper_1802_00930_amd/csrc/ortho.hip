@@ -289,7 +289,8 @@ struct MmArgs {
   int32_t pieces, per;     // of the reduction, of a slice
   int32_t slices;
   uint32_t tm, tn;
-  float* part;             // slices: [batch][tile][slice][quad][thread] of four sums
+  uint32_t tiles;          // of a matrix
+  float* part;             // slices: [batch][slice][tile][quad][thread] of four sums
   float unit;              // of the sum
   // outputs
   uint8_t *rowop, *colop;  // operand and (GRAM / POLY: the same) its transpose
@@ -308,22 +309,10 @@ struct MmArgs {
 
 enum { GRAM, POLY, STEP, LAST };
 
-// Tile (i, j), i <= j, of a triangle of t tiles a side.
-__device__ __forceinline__ void tri_tile(uint32_t id, uint32_t t, uint32_t* i, uint32_t* j) {
-  uint32_t row = 0, left = t;
-  while (id >= left) {
-    id -= left;
-    ++row;
-    --left;
-  }
-  *i = row;
-  *j = row + id;
-}
-
 template <int KIND>
 __device__ __forceinline__ void mm_tile(const MmArgs& g, uint32_t id, uint32_t* im, uint32_t* in) {
   if (KIND == GRAM || KIND == POLY)
-    tri_tile(id, g.tm, im, in);
+    tri_tile_of(id, g.tm, 8, im, in);
   else
     tile_of(id, g.tm, g.tn, 8, im, in);
 }
@@ -418,17 +407,20 @@ __device__ __forceinline__ void finish(const MmArgs& g, int64_t b, int64_t i0, i
 template <Prod P, int KIND, int T, bool MUON, bool SLICED, int TM, int TN, int WM, int WN, int S>
 __global__ __launch_bounds__(64 * WM * WN, 2) void k_mm(MmArgs g) {
   typedef MmaTile<P, TM, TN, WM, WN, S> Tile;
-  const int64_t b = blockIdx.y;
+  // matrices, their slices and those' tiles in order: an XCD's workgroups read few rows
+  // (12 of 512 x 512 dealt out one by one: every XCD reads every matrix)
+  const uint32_t id = xcd_order(blockIdx.x, gridDim.x), sl = id / g.tiles, tile = id - sl * g.tiles;
+  const int64_t b = SLICED ? sl / g.slices : sl;
+  const int32_t slice = SLICED ? sl % g.slices : 0;
   uint32_t im, in;
-  mm_tile<KIND>(g, SLICED ? blockIdx.x / g.slices : blockIdx.x, &im, &in);
-  const int32_t slice = SLICED ? blockIdx.x % g.slices : 0;
+  mm_tile<KIND>(g, tile, &im, &in);
   const int32_t p0 = slice * g.per, pieces = SLICED ? min(g.per, g.pieces - p0) : g.pieces;
   const int64_t i0 = (int64_t)im * TM, j0 = (int64_t)in * TN, at = (int64_t)p0 * kPiece;
   mv4f acc[Tile::FM][Tile::FN];
   Tile::run(g.a + b * g.sa + i0 * g.lda + at, g.lda, (int32_t)(g.m - i0), g.b + b * g.sb + j0 * g.ldb + at, g.ldb,
             (int32_t)(g.n - j0), pieces, acc);
   if (SLICED) {
-    mv4f* d = (mv4f*)g.part + (b * gridDim.x + blockIdx.x) * (int64_t)(TM * TN / 4) + threadIdx.x;
+    mv4f* d = (mv4f*)g.part + (int64_t)id * (TM * TN / 4) + threadIdx.x;
 #pragma unroll
     for (int j = 0; j < Tile::FN; ++j)
 #pragma unroll
@@ -462,10 +454,10 @@ __global__ __launch_bounds__(64 * WM * WN) void k_sum(MmArgs g) {
   const uint32_t id = blockIdx.x / (FN / 2), j = blockIdx.x % (FN / 2) * 2;
   uint32_t im, in;
   mm_tile<KIND>(g, id, &im, &in);
-  const int64_t tiles = gridDim.x / (FN / 2);
-  const mv4f* d = (const mv4f*)g.part + (b * tiles + id) * g.slices * (int64_t)(TM * TN / 4) + threadIdx.x;
+  const int64_t stride = (int64_t)g.tiles * (TM * TN / 4);  // of a slice
+  const mv4f* d = (const mv4f*)g.part + b * g.slices * stride + (int64_t)id * (TM * TN / 4) + threadIdx.x;
   float s[FM][8] = {};
-  for (int32_t k = 0; k < g.slices; ++k, d += TM * TN / 4) {
+  for (int32_t k = 0; k < g.slices; ++k, d += stride) {
     mv4f v[FM][2];
 #pragma unroll
     for (int i = 0; i < FM; ++i)
@@ -488,20 +480,21 @@ dfp_status launch_mm(int32_t id, const MmPlan& p, int32_t batch, MmArgs& g, hipS
   g.per = p.per;
   g.slices = p.slices;
   constexpr bool SYM = KIND == GRAM || KIND == POLY;
-  const uint32_t tiles = SYM ? g.tm * (g.tm + 1) / 2 : g.tm * g.tn;
+  g.tiles = SYM ? g.tm * (g.tm + 1) / 2 : g.tm * g.tn;
+  const uint32_t wgs = g.tiles * (uint32_t)batch;
   auto go = [&](auto side, auto wm, auto wn, auto s) -> dfp_status {
     constexpr int D = decltype(side)::value, WM = decltype(wm)::value, WN = decltype(wn)::value;
     constexpr int S = decltype(s)::value;
     const dim3 block(64 * WM * WN);
     if constexpr (SYM) {
       if (p.slices > 1) {
-        DFP_LAUNCH(id, (k_mm<P, KIND, T, MUON, true, D, D, WM, WN, S>), dim3(tiles * p.slices, (unsigned)batch), block,
-                   0, st, g);
-        DFP_LAUNCH(id, (k_sum<P, KIND, D, D, WM, WN>), dim3(tiles * (D / WN / 32), (unsigned)batch), block, 0, st, g);
+        DFP_LAUNCH(id, (k_mm<P, KIND, T, MUON, true, D, D, WM, WN, S>), dim3(wgs * p.slices), block, 0, st, g);
+        DFP_LAUNCH(id, (k_sum<P, KIND, D, D, WM, WN>), dim3(g.tiles * (D / WN / 32), (unsigned)batch), block, 0,
+                   st, g);
         return DFP_OK;
       }
     }
-    DFP_LAUNCH(id, (k_mm<P, KIND, T, MUON, false, D, D, WM, WN, S>), dim3(tiles, (unsigned)batch), block, 0, st, g);
+    DFP_LAUNCH(id, (k_mm<P, KIND, T, MUON, false, D, D, WM, WN, S>), dim3(wgs), block, 0, st, g);
     return DFP_OK;
   };
   typedef std::integral_constant<int, 2> Two;
