@@ -4,16 +4,18 @@
 //
 // The products read f16 operands in the layout of mma_tile.h: `gram` is X (or X^T
 // where R > C) with its longer side contiguous, `step` the other of the two; both
-// are written by the kernel that makes X.  BF16 results: operands of one f16 number,
-// X itself beside them in FP32, [R][C].  Otherwise: operands of a high and a low f16
-// part, and X is their sum (2^-24 of a value).  All sides are padded to 64 with
-// zeros, which every step keeps zero.
+// are written by the kernel that makes X.  X is held as the sum of two f16 numbers
+// (2^-24 of a value).  BF16 results: the operands are the high one alone, the low one
+// lies beside them, [R][C]; otherwise the operands have both.  All sides are padded
+// to 64 with zeros, which every step keeps zero.
 //
 // A and B are symmetric: only tiles on and above the diagonal are computed and each
-// is stored twice.  B's diagonal, the largest entries of its rows, stays out of the
-// f16 operand and joins in FP32: X = (a + B_ii) X + B' X.
+// is stored twice.  The diagonal of a I + B holds the largest entries of its rows: in
+// an operand of one f16 number it would be off by most, so it stays out of that and
+// joins in FP32, X = (a + B_ii) X + B' X; an operand of two takes it in, X = (a I + B) X,
+// and the step need not read X again.
 //
-// Units: X in 2^-12, A in 2^-10, B in 2^-sb so that |b A + c A A| <= 32768 in it
+// Units: X in 2^-12, A in 2^-10, B in 2^-sb so that |a I + b A + c A A| <= 32768 in it
 // for singular values up to sqrt(2).
 #include <algorithm>
 #include <cmath>
@@ -78,7 +80,7 @@ struct Plan {
   int64_t R, C, Rp, Cp;  // the matrix, padded
   int64_t r, rp;         // the smaller side, padded
   int64_t e;             // bytes of an operand element
-  int64_t x32, gram, step0, step1, aa, bb, diag, norm, slices, bytes;  // offsets, total
+  int64_t xlo, gram, step0, step1, aa, bb, diag, norm, slices, bytes;  // offsets, total
   MmPlan mgram, mpoly, mstep;
 };
 
@@ -103,13 +105,13 @@ Plan make_plan(const dfp_ortho_desc& d, bool split) {
   p.mgram = plan_mm(p.rp, p.rp, (p.tall ? p.Rp : p.Cp) / per_piece, d.batch, true, true, split);
   p.mpoly = plan_mm(p.rp, p.rp, p.rp / per_piece, d.batch, true, true, split);
   p.mstep = plan_mm(p.Rp, p.Cp, p.rp / per_piece, d.batch, false, false, split);
-  p.x32 = take(split ? 0 : n * 4);
+  p.xlo = take(split ? 0 : n * 2);
   p.gram = take(n * p.e);
   p.step0 = take(n * p.e);
   p.step1 = take(n * p.e);
   p.aa = take(s * p.e);
   p.bb = take(s * p.e);
-  p.diag = take(p.rp * d.batch * 4);
+  p.diag = take(split ? 0 : p.rp * d.batch * 4);
   p.norm = take((int64_t)kNormParts * d.batch * 8);
   p.slices = take(std::max(p.mgram.bytes, p.mpoly.bytes));
   p.bytes = at;
@@ -140,33 +142,33 @@ __device__ __forceinline__ void put4(uint8_t* p, int64_t k, const float (&v)[4])
   d[0] = make_uint2(hi[0] | hi[1] << 16, hi[2] | hi[3] << 16);
   if (P == Prod::F16X2) d[8] = make_uint2(lo[0] | lo[1] << 16, lo[2] | lo[3] << 16);
 }
+__device__ __forceinline__ uint4 pack8(const float (&v)[8]) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = h_bits((_Float16)v[2 * i]) | (uint32_t)h_bits((_Float16)v[2 * i + 1]) << 16;
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ uint4 pack8_low(const float (&v)[8]) {
+  float l[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) l[i] = v[i] - (float)(_Float16)v[i];
+  return pack8(l);
+}
 template <Prod P>
 __device__ __forceinline__ void put8(uint8_t* p, int64_t k, const float (&v)[8]) {
-  uint32_t hi[4], lo[4];
+  uint4* d = (uint4*)(p + op_off<P>(k));
+  d[0] = pack8(v);
+  if (P == Prod::F16X2) d[4] = pack8_low(v);
+}
+__device__ __forceinline__ void unpack8(const uint4& h, const uint4& l, float (&v)[8]) {
+  const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const _Float16 a = (_Float16)v[2 * i], b = (_Float16)v[2 * i + 1];
-    hi[i] = h_bits(a) | (uint32_t)h_bits(b) << 16;
-    lo[i] = h_bits((_Float16)(v[2 * i] - (float)a)) | (uint32_t)h_bits((_Float16)(v[2 * i + 1] - (float)b)) << 16;
-  }
-  uint4* d = (uint4*)(p + op_off<P>(k));
-  d[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-  if (P == Prod::F16X2) d[4] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-}
-template <Prod P>
-__device__ __forceinline__ void get8(const uint8_t* p, int64_t k, float (&v)[8]) {
-  const uint4* d = (const uint4*)(p + op_off<P>(k));
-  const uint4 h = d[0];
-  const uint32_t hw[4] = {h.x, h.y, h.z, h.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[2 * i] = h_val(hw[i]), v[2 * i + 1] = h_val(hw[i] >> 16);
-  if (P == Prod::F16X2) {
-    const uint4 l = d[4];
-    const uint32_t lw[4] = {l.x, l.y, l.z, l.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[2 * i] += h_val(lw[i]), v[2 * i + 1] += h_val(lw[i] >> 16);
+    v[2 * i] = h_val(hw[i]) + h_val(lw[i]);
+    v[2 * i + 1] = h_val(hw[i] >> 16) + h_val(lw[i] >> 16);
   }
 }
+
 // -------------------------------------------------------------------- norm
 // u = x (v null), or the momentum step on v in place and u from it.
 template <int T>
@@ -228,11 +230,11 @@ __global__ __launch_bounds__(kBlock) void k_norm(Source<T> s, int64_t n, double*
     part[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// X = u / (|u| + eps): both operands (and FP32), 64 x 64 tiles of the padded matrix.
+// X = u / (|u| + eps): both operands (and the low parts), 64 x 64 tiles of the padded matrix.
 template <int T, bool MUON, Prod P>
 __global__ __launch_bounds__(kBlock) void k_pack(Source<T> s, int64_t R, int64_t C, int64_t Rp, int64_t Cp,
                                                  const double* __restrict__ part, int32_t parts, float eps,
-                                                 float* __restrict__ x32, uint8_t* __restrict__ rowop,
+                                                 uint16_t* __restrict__ xlo, uint8_t* __restrict__ rowop,
                                                  uint8_t* __restrict__ colop) {
   __shared__ float tile[64][65];
   __shared__ double red[kBlock / 64];
@@ -261,15 +263,17 @@ __global__ __launch_bounds__(kBlock) void k_pack(Source<T> s, int64_t R, int64_t
     const int rr = (threadIdx.x >> 4) + i * 16;
     const int64_t r = r0 + rr, c = c0 + cc;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) u[i][j] = r < R && c + j < C ? (float)((double)u[i][j] * inv) : 0.f;
-    if (P == Prod::F16)
-      *(float4*)(x32 + (b * Rp + r) * Cp + c) = make_float4(u[i][0], u[i][1], u[i][2], u[i][3]);
-#pragma unroll
     for (int j = 0; j < 4; ++j) {
-      u[i][j] *= (float)(1 << kUnitX);
+      u[i][j] = r < R && c + j < C ? (float)((double)u[i][j] * inv) * (float)(1 << kUnitX) : 0.f;
       tile[rr][cc + j] = u[i][j];
     }
     put4<P>(rowop + b * pbytes + r * Cp * e, c, u[i]);
+    if (P == Prod::F16) {
+      uint16_t lo[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) lo[j] = h_bits((_Float16)(u[i][j] - (float)(_Float16)u[i][j]));
+      *(uint2*)(xlo + (b * Rp + r) * Cp + c) = make_uint2(lo[0] | (uint32_t)lo[1] << 16, lo[2] | (uint32_t)lo[3] << 16);
+    }
   }
   __syncthreads();
 #pragma unroll
@@ -295,11 +299,11 @@ struct MmArgs {
   // outputs
   uint8_t *rowop, *colop;  // operand and (GRAM / POLY: the same) its transpose
   int64_t ldr, ldc, sr, sc;
-  const uint8_t* old;      // POLY: A; STEP, LAST of two parts: X, in rowop's layout
-  float* diag;             // POLY writes, STEP reads, [rp] a matrix
+  const uint8_t* old;      // POLY: A; STEP, LAST of one part: X's high part; in rowop's layout
+  float* diag;             // one part: POLY writes, STEP reads, [rp] a matrix
   float cb, cc, ca;        // coefficients
   float uout;              // unit of the operands written
-  float* x32;              // one part: X
+  uint16_t* xlo;           // one part: X's low part
   int32_t R, C, rp;
   bool diag_cols;          // the diagonal goes by column (tall)
   void* out;
@@ -326,51 +330,63 @@ template <Prod P, int KIND, int T, bool MUON, int FM>
 __device__ __forceinline__ void finish(const MmArgs& g, int64_t b, int64_t i0, int64_t j0, bool mirror, uint16_t* lds,
                                        float (&s)[FM][8]) {
   constexpr int kRows = 16 * FM, kStride = kRows + 8;
+  constexpr bool ONE = P == Prod::F16, XSTEP = KIND == STEP || KIND == LAST;
   const int lane = threadIdx.x & 63;
-  const int64_t j = j0 + (lane >> 4) * 8;
+  const int64_t j = j0 + (lane >> 4) * 8, i1 = i0 + (lane & 15);
   const bool in_n = j < g.n;
+  // what the rows need from memory, all of it before the first is used
+  uint4 hi[FM], lo[FM];
+  float w[FM][8], dg[FM];
 #pragma unroll
   for (int fi = 0; fi < FM; ++fi) {
-    const int64_t i = i0 + fi * 16 + (lane & 15);
+    const int64_t i = i1 + fi * 16;
+    hi[fi] = lo[fi] = make_uint4(0, 0, 0, 0);
+    dg[fi] = 0.f;
+    if (i >= g.m || !in_n) continue;
+    if (KIND == POLY || (XSTEP && ONE)) {
+      const uint4* d = (const uint4*)(g.old + b * g.sr + i * g.ldr + op_off<P>(j));
+      hi[fi] = d[0];
+      if (KIND == POLY && !ONE) lo[fi] = d[4];
+      if (XSTEP) lo[fi] = *(const uint4*)(g.xlo + (b * g.m + i) * (int64_t)g.n + j);
+    }
+    if (XSTEP && ONE && !g.diag_cols) dg[fi] = g.diag[b * g.rp + i];
+    if (KIND == LAST && MUON && i < g.R && j < g.C) load_n<DFP_F32, 8>(g.w + (b * g.R + i) * g.C + j, g.C - j, w[fi]);
+  }
+  float dc[8] = {};
+  if (XSTEP && ONE && g.diag_cols && in_n) load_n<DFP_F32, 8>(g.diag + b * g.rp + j, dc);
+#pragma unroll
+  for (int fi = 0; fi < FM; ++fi) {
+    const int64_t i = i1 + fi * 16;
     float(&v)[8] = s[fi];
     if (i >= g.m || !in_n) continue;
 #pragma unroll
     for (int r = 0; r < 8; ++r) v[r] *= g.unit;
+    float x[8];
+    if (KIND == POLY || (XSTEP && ONE)) unpack8(hi[fi], lo[fi], x);
     if (KIND == POLY) {
-      float a[8];
-      get8<P>(g.old + b * g.sr + i * g.ldr, j, a);
 #pragma unroll
       for (int r = 0; r < 8; ++r) {
-        v[r] = fmaf(g.cc, v[r], g.cb * (a[r] * (1.f / (1 << kUnitA))));
+        v[r] = fmaf(g.cc, v[r], g.cb * (x[r] * (1.f / (1 << kUnitA))));
         if (i == j + r) {
-          g.diag[b * g.rp + i] = v[r];
-          v[r] = 0.f;
+          v[r] += g.ca;
+          if (ONE) {
+            g.diag[b * g.rp + i] = v[r];
+            v[r] = 0.f;
+          }
         }
       }
     }
-    if (KIND == STEP || KIND == LAST) {
-      float x[8];
-      float* px = g.x32 + (b * g.m + i) * (int64_t)g.n + j;
-      if (P == Prod::F16) {
-        load_n<DFP_F32, 8>(px, x);
-      } else {
-        get8<P>(g.old + b * g.sr + i * g.ldr, j, x);
+    if (XSTEP && ONE) {
 #pragma unroll
-        for (int r = 0; r < 8; ++r) x[r] *= 1.f / (1 << kUnitX);
-      }
-#pragma unroll
-      for (int r = 0; r < 8; ++r) v[r] = fmaf(g.ca + g.diag[b * g.rp + (g.diag_cols ? j + r : i)], x[r], v[r]);
-      if (KIND == STEP && P == Prod::F16) store_n<DFP_F32, 8>(px, v);
+      for (int r = 0; r < 8; ++r) v[r] = fmaf(g.diag_cols ? dc[r] : dg[fi], x[r] * (1.f / (1 << kUnitX)), v[r]);
     }
     if (KIND == LAST) {
       if (i >= g.R || j >= g.C) continue;
       const int64_t at = (b * g.R + i) * g.C + j;
       if (MUON) {
-        float w[8];
-        load_n<DFP_F32, 8>(g.w + at, g.C - j, w);
 #pragma unroll
-        for (int r = 0; r < 8; ++r) w[r] = fmaf(-g.alpha, v[r], g.keep * w[r]);
-        store_n<DFP_F32, 8>(g.w + at, g.C - j, w);
+        for (int r = 0; r < 8; ++r) w[fi][r] = fmaf(-g.alpha, v[r], g.keep * w[fi][r]);
+        store_n<DFP_F32, 8>(g.w + at, g.C - j, w[fi]);
       } else {
         store_n<T, 8>((typename Elem<T>::type*)g.out + at, g.C - j, v);
       }
@@ -379,6 +395,7 @@ __device__ __forceinline__ void finish(const MmArgs& g, int64_t b, int64_t i0, i
 #pragma unroll
     for (int r = 0; r < 8; ++r) v[r] *= g.uout;
     put8<P>(g.rowop + b * g.sr + i * g.ldr, j, v);
+    if (KIND == STEP && ONE) *(uint4*)(g.xlo + (b * g.m + i) * (int64_t)g.n + j) = pack8_low(v);
   }
   if (KIND == LAST || !mirror) return;
   // (g.m is a multiple of 64: a wave's rows are all in or, from kRows = 64 on, all out)
@@ -503,9 +520,9 @@ dfp_status launch_mm(int32_t id, const MmPlan& p, int32_t batch, MmArgs& g, hipS
   return go(std::integral_constant<int, 64>(), Two(), Two(), std::integral_constant<int, 3>());
 }
 
-// Largest unit of B that keeps |b A + c A A| at 32768 or less for |X| <= sqrt(2).
+// Largest unit of a I + B that keeps it at 32768 or less for |X| <= sqrt(2).
 float unit_b(const float* coef) {
-  const double most = std::fabs((double)coef[1]) * 2. + std::fabs((double)coef[2]) * 4.;
+  const double most = std::fabs((double)coef[0]) + std::fabs((double)coef[1]) * 2. + std::fabs((double)coef[2]) * 4.;
   int s = 12;
   while (s > 0 && most * (double)(1 << s) > 32768.) --s;
   return (float)(1 << s);
@@ -518,7 +535,7 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
   constexpr int64_t kPerPiece = SPLIT ? 32 : 64;  // elements of a piece
   const Plan p = make_plan(d, SPLIT);
   uint8_t* base = (uint8_t*)ws;
-  float* x32 = (float*)(base + p.x32);
+  uint16_t* xlo = (uint16_t*)(base + p.xlo);
   uint8_t *gram = base + p.gram, *aa = base + p.aa, *bb = base + p.bb;
   uint8_t* step[2] = {base + p.step0, base + p.step1};
   double* part = (double*)(base + p.norm);
@@ -530,7 +547,7 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
   uint8_t* rowop = p.tall ? step[0] : gram;
   uint8_t* colop = p.tall ? gram : step[0];
   DFP_LAUNCH(K_ORTHO_PACK, (k_pack<T, MUON, P>), dim3((unsigned)(p.Rp / 64 * (p.Cp / 64)), nb), dim3(kBlock), 0, st,
-             src, p.R, p.C, p.Rp, p.Cp, part, parts, d.eps, x32, rowop, colop);
+             src, p.R, p.C, p.Rp, p.Cp, part, parts, d.eps, xlo, rowop, colop);
   const int64_t longer = p.tall ? p.Rp : p.Cp;
   const int64_t sx = p.Rp * p.Cp * p.e, ss = p.rp * p.rp * p.e;
   constexpr float kInvX = 1.f / (1 << kUnitX), kInvA = 1.f / (1 << kUnitA);
@@ -554,7 +571,7 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
     g.ldr = g.ldc = p.rp * p.e;
     g.sr = g.sc = ss;
     if ((rc = launch_mm<P, GRAM, 0, false>(K_ORTHO_GRAM, p.mgram, d.batch, g, st)) != DFP_OK) return rc;
-    // B = b A + c A A
+    // B = b A + c A A (and a on its diagonal)
     g.a = g.b = g.old = aa;
     g.lda = g.ldb = p.rp * p.e;
     g.sa = g.sb = ss;
@@ -563,7 +580,7 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
     g.uout = ub;
     g.rowop = g.colop = bb;
     if ((rc = launch_mm<P, POLY, 0, false>(K_ORTHO_POLY, p.mpoly, d.batch, g, st)) != DFP_OK) return rc;
-    // X = a X + B X, in the caller's orientation: rows of B by rows of X^T, or rows of X by rows of B
+    // X = (a I + B) X, in the caller's orientation: rows of B by rows of X^T, or rows of X by rows of B
     uint8_t *from = step[s & 1], *to = step[(s + 1) & 1];
     g.a = p.tall ? from : bb;
     g.b = p.tall ? bb : from;
@@ -577,7 +594,7 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
     g.old = p.tall ? from : gram;
     g.ldr = p.Cp * p.e, g.ldc = p.Rp * p.e;
     g.sr = g.sc = sx;
-    g.x32 = x32;
+    g.xlo = xlo;
     g.R = (int32_t)p.R, g.C = (int32_t)p.C;
     g.diag_cols = p.tall;
     g.out = out;
