@@ -17,13 +17,21 @@ struct I8Scale {
   float s, su, inv, up;
   bool live;
 };
-__device__ __forceinline__ I8Scale i8_scale(uint32_t amax_bits) {
+// Scale s with the reciprocal that i8_scale found for it (0: the row's integers are 0).
+__device__ __forceinline__ I8Scale i8_scale_of(float s, float inv) {
   I8Scale r;
+  r.s = s;
+  r.live = inv != 0.f;
+  r.up = s < 0x1p-60f ? 0x1p64f : 1.f;
+  r.su = s * r.up;
+  r.inv = inv;
+  return r;
+}
+__device__ __forceinline__ I8Scale i8_scale(uint32_t amax_bits) {
   const bool finite = amax_bits < 0x7f800000u;
-  r.s = finite ? __uint_as_float(amax_bits) / 127.f : __uint_as_float(0x7fc00000u);
-  r.live = finite && r.s > 0.f;
-  r.up = r.s < 0x1p-60f ? 0x1p64f : 1.f;
-  r.su = r.s * r.up;
+  const float s = finite ? __uint_as_float(amax_bits) / 127.f : __uint_as_float(0x7fc00000u);
+  I8Scale r = i8_scale_of(s, 0.f);
+  r.live = finite && s > 0.f;
   r.inv = r.live ? 1.f / r.su : 0.f;
   return r;
 }
@@ -47,8 +55,10 @@ __device__ __forceinline__ int32_t i8_round(float x, const I8Scale& k, uint32_t 
   return (int32_t)fminf(fmaxf(q, -127.f), 127.f);
 }
 
-__device__ __forceinline__ uint32_t pack4(int32_t a, int32_t b, int32_t c, int32_t d) {
-  return (a & 0xff) | ((b & 0xff) << 8) | ((c & 0xff) << 16) | ((uint32_t)d << 24);
+// The low bytes of four words.
+__device__ __forceinline__ uint32_t low_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400u), __builtin_amdgcn_perm(b, a, 0x0c0c0400u),
+                               0x05040100u);
 }
 
 // Philox words of N consecutive flat indices.
@@ -68,15 +78,39 @@ __device__ __forceinline__ void words(uint64_t idx, uint32_t k0, uint32_t k1, ui
   }
 }
 
+// The nearest integers of eight elements with scales k[i] (or one for all, k[0]), two
+// bytes' worth of answers at a time in the common case: r = x inv + 1.5 2^23 rounds x inv to
+// an integer and holds it in its low byte.  x inv is off from x / s by at most 127
+// 2^-23, so the integer is right unless it is that near to a tie, d = 1/2; then, and
+// for subnormal scales, the exact rounding above.  Memory's rate leaves about 20
+// operations an element: the exact rounding alone takes them all (16384 x 8192 BF16
+// 108 us by it).
+template <bool EACH>
+__device__ __forceinline__ bool i8_nearest8(const float (&v)[8], const I8Scale* k, uint32_t (&o)[8]) {
+  float far = 0.f;
+  bool plain = true;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const I8Scale& s = k[EACH ? i : 0];
+    const float r = fmaf(v[i], s.inv, 12582912.f), d = fmaf(v[i], s.inv, 12582912.f - r);
+    far = fmaxf(far, fabsf(d));
+    if (EACH || i == 0) plain = plain && s.up == 1.f;
+    o[i] = __float_as_uint(r);
+  }
+  return plain && far < 0.49998f;
+}
+
 template <int MODE>
 __device__ __forceinline__ uint2 i8_round8(const float (&v)[8], const I8Scale& k, uint64_t idx, uint32_t k0,
                                            uint32_t k1, uint32_t role) {
-  uint32_t u[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  if (MODE == DFP_ROUND_STOCHASTIC) words<8>(idx, k0, k1, role, u);
-  int32_t q[8];
+  uint32_t q[8];
+  if (MODE != DFP_ROUND_NEAREST || !i8_nearest8<false>(v, &k, q)) {
+    uint32_t u[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (MODE == DFP_ROUND_STOCHASTIC) words<8>(idx, k0, k1, role, u);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) q[i] = i8_round<MODE>(v[i], k, u[i]);
-  const uint2 o = make_uint2(pack4(q[0], q[1], q[2], q[3]), pack4(q[4], q[5], q[6], q[7]));
+    for (int i = 0; i < 8; ++i) q[i] = (uint32_t)i8_round<MODE>(v[i], k, u[i]);
+  }
+  const uint2 o = make_uint2(low_bytes(q[0], q[1], q[2], q[3]), low_bytes(q[4], q[5], q[6], q[7]));
   return k.live ? o : make_uint2(0, 0);
 }
 

@@ -102,13 +102,15 @@ __device__ __forceinline__ void transpose4(const uint32_t (&w)[4], uint32_t (&o)
   o[3] = __builtin_amdgcn_perm(d, c, 0x07060302u);
 }
 
-// The transposed tile in LDS: 128 columns of 32 words (128 tokens), written out as
+// The transposed tile in LDS: COLS columns of 32 words (128 tokens), written out as
 // rows of 128 bytes.  33 words a column keep both directions off shared banks.
-typedef uint32_t TileT[128][33];
-__device__ __forceinline__ void store_tile_t(const TileT& tile, int8_t* qt, int64_t cols, int64_t ldt, int64_t r0,
-                                             int64_t c0) {
+template <int COLS>
+using TileT = uint32_t[COLS][33];
+template <int COLS>
+__device__ __forceinline__ void store_tile_t(const TileT<COLS>& tile, int8_t* qt, int64_t cols, int64_t ldt,
+                                             int64_t r0, int64_t c0) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < COLS / 32; ++i) {
     const int c = (threadIdx.x >> 3) + i * 32, w = (threadIdx.x & 7) * 4;
     if (c0 + c < cols)
       *reinterpret_cast<uint4*>(qt + (c0 + c) * ldt + r0 + w * 4) =
@@ -120,7 +122,7 @@ __device__ __forceinline__ void store_tile_t(const TileT& tile, int8_t* qt, int6
 __global__ __launch_bounds__(kBlock) void k_transpose_i8(const int8_t* __restrict__ q, int64_t rows, int64_t cols,
                                                          int64_t ld, int8_t* __restrict__ qt, int64_t ldt,
                                                          uint32_t ctiles) {
-  __shared__ TileT tile;
+  __shared__ TileT<128> tile;
   const int64_t r0 = (int64_t)(blockIdx.x / ctiles) * 128, c0 = (int64_t)(blockIdx.x % ctiles) * 128;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -136,7 +138,7 @@ __global__ __launch_bounds__(kBlock) void k_transpose_i8(const int8_t* __restric
     for (int j = 0; j < 4; ++j) tile[c4 * 4 + j][r4] = o[j];
   }
   __syncthreads();
-  store_tile_t(tile, qt, cols, ldt, r0, c0);
+  store_tile_t<128>(tile, qt, cols, ldt, r0, c0);
 }
 
 // Column maxima of |x[r][c] roww[r]| and column sums of x over slices of the rows:
@@ -153,17 +155,22 @@ __global__ __launch_bounds__(kBlock) void k_col_max(const typename Elem<T>::type
   const int64_t r1 = min(rows, (part + 1) * slice);
   uint32_t mx[8] = {};
   float sum[8] = {};
-  for (int64_t r = part * slice + rg; r < r1; r += 8) {
-    float v[8];
-    if (c < cols) load_n<T, 8>(src + r * cols + c, cols - c, v);
-    else
-      for (int i = 0; i < 8; ++i) v[i] = 0.f;
-    const float w = roww[r];
+  constexpr int U = 4;  // rows in flight
+  for (int64_t r = part * slice + rg; r < r1; r += 8 * U) {
+    float v[U][8], w[U];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      mx[i] = max(mx[i], __float_as_uint(v[i] * w) & 0x7fffffffu);
-      sum[i] += v[i];
+    for (int u = 0; u < U; ++u) {
+      const bool in = r + u * 8 < r1;
+      w[u] = in ? roww[r + u * 8] : 0.f;
+      load_n<T, 8>(src + (r + u * 8) * cols + c, in ? cols - c : 0, v[u]);
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        mx[i] = max(mx[i], __float_as_uint(v[u][i] * w[u]) & 0x7fffffffu);
+        sum[i] += v[u][i];
+      }
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -185,60 +192,92 @@ __global__ __launch_bounds__(kBlock) void k_col_max(const typename Elem<T>::type
   }
 }
 
-// Scales of the columns (and their sums) from the slices, in slice order.
+// Scales of the columns (and their sums) from the slices: 64 columns a workgroup, its
+// four waves every fourth slice, the waves' results in order.
 __global__ __launch_bounds__(kBlock) void k_col_scale(const uint32_t* __restrict__ pmax, const float* __restrict__ psum,
                                                       int32_t parts, int64_t cols, float* __restrict__ scale,
-                                                      uint32_t* __restrict__ amax, float* __restrict__ sums) {
-  const int64_t c = (int64_t)blockIdx.x * kBlock + threadIdx.x;
-  if (c >= cols) return;
+                                                      float* __restrict__ inv, float* __restrict__ sums) {
+  __shared__ uint32_t wm[4][64];
+  __shared__ float wsum[4][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t c = (int64_t)blockIdx.x * 64 + lane, at = min(c, cols - 1);
   uint32_t m = 0;
   float s = 0.f;
-  for (int32_t p = 0; p < parts; ++p) {
-    m = max(m, pmax[(int64_t)p * cols + c]);
-    s += psum[(int64_t)p * cols + c];
+  for (int32_t p = wave; p < parts; p += 32) {  // eight loads in flight
+    uint32_t vm[8];
+    float vs[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int64_t o = (int64_t)min(p + u * 4, parts - 1) * cols + at;
+      vm[u] = pmax[o];
+      vs[u] = psum[o];
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (p + u * 4 < parts) {
+        m = max(m, vm[u]);
+        s += vs[u];
+      }
   }
-  scale[c] = i8_scale(m).s;
-  amax[c] = m;
-  if (sums) sums[c] = s;
+  wm[wave][lane] = m;
+  wsum[wave][lane] = s;
+  __syncthreads();
+  if (wave || c >= cols) return;
+  m = max(max(m, wm[1][lane]), max(wm[2][lane], wm[3][lane]));
+  const I8Scale k = i8_scale(m);
+  scale[c] = k.s;
+  inv[c] = k.inv;
+  if (sums) sums[c] = (s + wsum[1][lane]) + (wsum[2][lane] + wsum[3][lane]);
 }
 
-// x[r][c] roww[r] rounded by column scale into qt [cols][ldt]: 128 x 128 tiles,
-// a thread 4 rows x 8 columns at a time.
+// x[r][c] roww[r] rounded by column scale into qt [cols][ldt]: tiles of 128 rows x
+// 64 columns, a thread 4 x 8 of them.
 template <int T, int MODE>
 __global__ __launch_bounds__(kBlock) void k_col_i8_t(const typename Elem<T>::type* __restrict__ src, int64_t rows,
                                                      int64_t cols, const float* __restrict__ roww,
-                                                     const uint32_t* __restrict__ amax, int8_t* __restrict__ qt,
+                                                     const float* __restrict__ scale,
+                                                     const float* __restrict__ inv, int8_t* __restrict__ qt,
                                                      int64_t ldt, uint32_t ctiles, uint32_t k0, uint32_t k1,
                                                      uint32_t role) {
-  __shared__ TileT tile;
-  const int64_t r0 = (int64_t)(blockIdx.x / ctiles) * 128, c0 = (int64_t)(blockIdx.x % ctiles) * 128;
-  const int c8 = threadIdx.x & 15;
+  __shared__ TileT<64> tile;
+  const int64_t r0 = (int64_t)(blockIdx.x / ctiles) * 128, c0 = (int64_t)(blockIdx.x % ctiles) * 64;
+  const int c8 = threadIdx.x & 7, r4 = threadIdx.x >> 3;
   const int64_t c = c0 + c8 * 8;
+  float ks[8], ki[8];
+  load_n<DFP_F32, 8>(scale + c, cols - c, ks);
+  load_n<DFP_F32, 8>(inv + c, cols - c, ki);
   I8Scale k[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) k[i] = i8_scale(c + i < cols ? amax[c + i] : 0u);
+  for (int i = 0; i < 8; ++i) k[i] = i8_scale_of(ks[i], ki[i]);
+  float v[4][8];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int r4 = (threadIdx.x >> 4) + h * 16;
-    uint32_t o[8] = {};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int64_t r = r0 + r4 * 4 + j;
-      if (r >= rows || c >= cols) continue;
-      float v[8];
-      load_n<T, 8>(src + r * cols + c, cols - c, v);
+  for (int j = 0; j < 4; ++j) {
+    const int64_t r = r0 + r4 * 4 + j;
+    if (r < rows && c < cols) {
+      load_n<T, 8>(src + r * cols + c, cols - c, v[j]);
       const float w = roww[r];
-      uint32_t u[8] = {};
-      if (MODE == DFP_ROUND_STOCHASTIC) words<8>(r * cols + c, k0, k1, role, u);
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (k[i].live) o[i] |= (uint32_t)(i8_round<MODE>(v[i] * w, k[i], u[i]) & 0xff) << (8 * j);
+      for (int i = 0; i < 8; ++i) v[j][i] *= w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[j][i] = 0.f;
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) tile[c8 * 8 + i][r4] = o[i];
   }
+  uint32_t q[4][8];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    if (MODE == DFP_ROUND_NEAREST && i8_nearest8<true>(v[j], k, q[j])) continue;
+    uint32_t u[8] = {};
+    if (MODE == DFP_ROUND_STOCHASTIC) words<8>((r0 + r4 * 4 + j) * cols + c, k0, k1, role, u);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[j][i] = (uint32_t)i8_round<MODE>(v[j][i], k[i], u[i]);
+  }
+  // (a row past the last is a row of zeros: its words are never above F = 0)
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    tile[c8 * 8 + i][r4] = k[i].live ? low_bytes(q[0][i], q[1][i], q[2][i], q[3][i]) : 0u;
   __syncthreads();
-  store_tile_t(tile, qt, cols, ldt, r0, c0);
+  store_tile_t<64>(tile, qt, cols, ldt, r0, c0);
 }
 
 constexpr int64_t kMaxBlocks = 1 << 22;  // of a grid-stride launch
@@ -264,9 +303,11 @@ dfp_status launch_rows_i8(int32_t type, int32_t rounding, uint64_t seed, uint32_
       auto by_len = [&](auto weighted) -> dfp_status {
         typedef std::integral_constant<int, 64> Wave;
         typedef std::integral_constant<int, 256> Group;
-        // the shortest register row that holds it: a wave up to 1024, a workgroup up to 16384
+        // a wave a row up to 2048 (8192 x 2048 BF16 9.8 us; by workgroups 15.6), or 16 waves for a
+        // few long rows, a workgroup up to 16384
         if (nvec <= 64) return go(Wave(), std::integral_constant<int, 1>(), weighted);
         if (nvec <= 128) return go(Wave(), std::integral_constant<int, 2>(), weighted);
+        if (nvec <= 256 && rows > 512) return go(Wave(), std::integral_constant<int, 4>(), weighted);
         if (nvec <= 256) return go(Group(), std::integral_constant<int, 1>(), weighted);
         if (nvec <= 512) return go(Group(), std::integral_constant<int, 2>(), weighted);
         if (nvec <= 1024) return go(Group(), std::integral_constant<int, 4>(), weighted);
@@ -288,8 +329,8 @@ dfp_status launch_transpose_i8(const int8_t* q, int64_t rows, int64_t cols, int8
 ColPlan plan_cols_i8(int64_t rows, int64_t cols) {
   ColPlan p;
   const int64_t cb = (cols + 255) / 256;
-  // enough slices for four workgroups a CU, of at least 64 rows
-  int64_t parts = std::max<int64_t>(1, std::min<int64_t>((rows + 63) / 64, 1024 / cb));
+  // enough slices for four workgroups a CU, of at least 32 rows
+  int64_t parts = std::max<int64_t>(1, std::min<int64_t>((rows + 31) / 32, 1024 / cb));
   p.slice = (rows + parts - 1) / parts;
   p.parts = (rows + p.slice - 1) / p.slice;
   p.bytes = (p.parts * 2 + 1) * cols * 4;
@@ -302,20 +343,20 @@ dfp_status launch_cols_i8_t(int32_t type, int32_t rounding, uint64_t seed, uint3
   const ColPlan p = plan_cols_i8(rows, cols);
   uint32_t* pmax = (uint32_t*)ws;
   float* psum = (float*)(pmax + p.parts * cols);
-  uint32_t* amax = (uint32_t*)(psum + p.parts * cols);
+  float* inv = psum + p.parts * cols;
   const uint32_t cb = (uint32_t)((cols + 255) / 256);
   const uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
-  const int64_t rt = (rows + 127) / 128, ct = (cols + 127) / 128;
+  const int64_t rt = (rows + 127) / 128, ct = (cols + 63) / 64;
   return with_type(type, [&](auto tc) -> dfp_status {
     constexpr int T = decltype(tc)::value;
     typedef const typename Elem<T>::type* S;
     DFP_LAUNCH(K_I8_COLS, k_col_max<T>, dim3((unsigned)(cb * p.parts)), dim3(kBlock), 0, st, (S)src, rows, cols, roww,
                p.slice, cb, pmax, psum);
-    DFP_LAUNCH(K_I8_COLS, k_col_scale, dim3((unsigned)((cols + kBlock - 1) / kBlock)), dim3(kBlock), 0, st, pmax, psum,
-               (int32_t)p.parts, cols, scale, amax, sums);
+    DFP_LAUNCH(K_I8_COLS, k_col_scale, dim3((unsigned)((cols + 63) / 64)), dim3(kBlock), 0, st, pmax, psum,
+               (int32_t)p.parts, cols, scale, inv, sums);
     return with_mode(rounding, [&](auto mc) -> dfp_status {
       DFP_LAUNCH(K_I8_COLS, (k_col_i8_t<T, decltype(mc)::value>), dim3((unsigned)(rt * ct)), dim3(kBlock), 0, st,
-                 (S)src, rows, cols, roww, amax, qt, i8_ld(rows), (uint32_t)ct, k0, k1, role);
+                 (S)src, rows, cols, roww, scale, inv, qt, i8_ld(rows), (uint32_t)ct, k0, k1, role);
       return DFP_OK;
     });
   });
