@@ -24,7 +24,7 @@ dfp_status launch_cols_i8_t(int32_t type, int32_t rounding, uint64_t seed, uint3
 
 // out [m][n] (type) = (sum over k of a b) sa[m] sb[n] + bias[n]; sb, bias nullable.  ws: plan_gemm_i8(...).bytes.
 struct I8Plan {
-  int32_t side;         // of the output tiles; 0: the kernel for few rows
+  int32_t kind;         // of tile (mma_tile.h); -1: the kernel for few rows
   int32_t slices, per;  // of the reduction, pieces in each
   int64_t bytes;        // the slices' sums
 };

@@ -267,44 +267,37 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_token(I8Args g, const typena
 // The kernel of a product by an estimate of its time (us).
 //   k_few    a CU takes 0.15, 0.21 or 0.35 for a piece of 16 columns by up to 16, 32
 //            or 64 rows (4096 x 4096, 8192 x 2048 and 8192 x 8192 weights).
-//   k_tiles  a piece of a tile takes `alone` if a CU has one tile and `busy` a tile
-//            if it has several (512 x 512 x 8192 and 8192^3); with weights that come
-//            from memory, as they do for few rows, a quarter more.  Slices mean that
-//            their sums are written and read (4 TB/s) and a second kernel (4).
+//   k_tiles  tile_us; with weights that come from memory, as they do for few rows, a
+//            quarter more.  Slices mean that their sums are written and read (4 TB/s)
+//            and a second kernel (4).
 // At 64 rows: 4096 x 4096 k_few 13.8, tiles 12.7; 8192 x 2048 13.4 and 9.2; 8192 x
 // 8192 44 and 22; 1024 x 1024 5.0 and 5.2.  At 24: 9.6 and 13.6; 8.5 and 8.8; 25.5 and
 // 18.8; 3.6 and 4.8.
-struct TileKind {
-  int32_t side;
-  double alone, busy;
-};
-constexpr TileKind kKinds[] = {{256, 1.38, 1.74}, {128, 0.57, 0.58}, {64, 0.29, 0.18}};
 constexpr int32_t kFewRows = 64;
 constexpr int64_t kMostPartBytes = 64 << 20;
 
 }  // namespace
 
 I8Plan plan_gemm_i8(int64_t m, int64_t n, int64_t k) {
-  I8Plan best{};
+  I8Plan best{-1, 1, 0, 0};
   const int64_t pieces = i8_ld(k) / kPiece;
   double least = 1e30;
   if (m <= kFewRows) {
     least = 2. + ((n + 15) / 16 + 255) / 256 * pieces * (m <= 16 ? 0.15 : m <= 32 ? 0.21 : 0.35);
     if (m <= 16) return best;
   }
-  for (int t = 0; t < 3; ++t) {
-    const TileKind& kind = kKinds[t];
-    const int64_t tiles = ((m + kind.side - 1) / kind.side) * ((n + kind.side - 1) / kind.side);
+  for (int t = 0; t < kTileKindCount; ++t) {
+    const TileKind& kind = kTileKinds[t];
+    const int64_t tiles = ((m + kind.tm - 1) / kind.tm) * ((n + kind.tn - 1) / kind.tn);
     for (int64_t slices = 1; slices <= 16 && slices <= pieces; slices *= 2) {
       const int64_t per = (pieces + slices - 1) / slices, used = (pieces + per - 1) / per;
       const int64_t bytes = used > 1 ? used * m * n * 4 : 0;
       if (bytes > kMostPartBytes) break;
-      const int64_t a_cu = (tiles * used + 255) / 256;
-      double us = 2.5 + per * std::max(kind.alone, a_cu * kind.busy) * (m <= kFewRows ? 1.25 : 1.);
+      double us = 2.5 + tile_us(kind, false, tiles * used, per) * (m <= kFewRows ? 1.25 : 1.);
       if (used > 1) us += 4. + 2. * bytes / 4e6;
       if (us < least) {
         least = us;
-        best = {kind.side, (int32_t)used, (int32_t)per, bytes};
+        best = {t, (int32_t)used, (int32_t)per, bytes};
       }
     }
   }
@@ -336,7 +329,7 @@ dfp_status launch_gemm_i8(int32_t m, int32_t n, int32_t k, const int8_t* a, cons
   I8Args g{(const uint8_t*)a, (const uint8_t*)b, sa, sb, bias, out, (int32_t*)ws, i8_ld(k), m, n, 0, 0, p.per};
   return with_type(type, [&](auto tc) -> dfp_status {
     constexpr int T = decltype(tc)::value;
-    if (!p.side) {
+    if (p.kind < 0) {
       const dim3 grid((unsigned)(((int64_t)n + 15) / 16)), block(64 * kFewWaves);
       if (m <= 16)
         DFP_LAUNCH(K_I8_GEMM, (k_few<T, 1, 4>), grid, block, 0, st, g);
@@ -346,20 +339,18 @@ dfp_status launch_gemm_i8(int32_t m, int32_t n, int32_t k, const int8_t* a, cons
         DFP_LAUNCH(K_I8_GEMM, (k_few<T, 4, 4>), grid, block, 0, st, g);
       return DFP_OK;
     }
-    g.tm = (uint32_t)(((int64_t)m + p.side - 1) / p.side);
-    g.tn = (uint32_t)(((int64_t)n + p.side - 1) / p.side);
+    g.tm = (uint32_t)(((int64_t)m + kTileKinds[p.kind].tm - 1) / kTileKinds[p.kind].tm);
+    g.tn = (uint32_t)(((int64_t)n + kTileKinds[p.kind].tn - 1) / kTileKinds[p.kind].tn);
     auto tiles = [&](auto sliced) -> dfp_status {
       constexpr bool SL = decltype(sliced)::value;
-      const dim3 grid(g.tm * g.tn * (unsigned)p.slices);
       // (a sliced kernel stores integers: one instance serves every type)
       constexpr int TT = SL ? DFP_F32 : T;
-      if (p.side == 256)
-        DFP_LAUNCH(K_I8_GEMM, (k_tiles<TT, SL, 256, 256, 4, 2, 2>), grid, dim3(512), 0, st, g);
-      else if (p.side == 128)
-        DFP_LAUNCH(K_I8_GEMM, (k_tiles<TT, SL, 128, 128, 2, 2, 2>), grid, dim3(256), 0, st, g);
-      else
-        DFP_LAUNCH(K_I8_GEMM, (k_tiles<TT, SL, 64, 64, 2, 2, 3>), grid, dim3(256), 0, st, g);
-      return DFP_OK;
+      return with_tile(p.kind, [&](auto shape) -> dfp_status {
+        typedef decltype(shape) Q;
+        DFP_LAUNCH(K_I8_GEMM, (k_tiles<TT, SL, Q::TM, Q::TN, Q::WM, Q::WN, Q::S>),
+                   dim3(g.tm * g.tn * (unsigned)p.slices), dim3(64 * Q::WM * Q::WN), 0, st, g);
+        return DFP_OK;
+      });
     };
     if (p.slices == 1) return tiles(std::false_type());
     const dfp_status rc = tiles(std::true_type());

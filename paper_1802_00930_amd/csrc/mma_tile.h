@@ -186,6 +186,41 @@ struct MmaTile {
   }
 };
 
+// The tiles in use, and a CU's time for a piece of one: `alone` if it has one tile,
+// `busy` a tile if it has several (us; I8 and F16, F16X2; 512 x 512 x 8192 bytes and
+// 8192^2 x 8192).  Outputs of a tile per time fall with its side, but a product takes
+// as long as the CU with the most tiles, and 256 CUs are filled in steps: 3008 x 3008
+// x 4096 takes 63.6, 42.7, 46.8, 55.0, 59.1 and 65.3 with these.
+template <int TM_, int TN_, int WM_, int WN_, int S_>
+struct TileShape {
+  static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, S = S_;
+};
+struct TileKind {
+  int32_t tm, tn;
+  double alone[2], busy[2];
+};
+constexpr TileKind kTileKinds[] = {
+    {256, 256, {1.38, 1.74}, {1.78, 2.22}}, {192, 192, {0.85, 1.05}, {1.14, 1.42}},
+    {192, 128, {0.67, 0.75}, {0.67, 0.88}}, {128, 128, {0.58, 0.64}, {0.58, 0.62}},
+    {96, 96, {0.39, 0.44}, {0.39, 0.46}},   {64, 64, {0.31, 0.33}, {0.18, 0.20}},
+};
+constexpr int kTileKindCount = 6;
+template <class F>
+dfp_status with_tile(int32_t kind, F f) {
+  switch (kind) {
+    case 0: return f(TileShape<256, 256, 4, 2, 2>());
+    case 1: return f(TileShape<192, 192, 4, 2, 2>());
+    case 2: return f(TileShape<192, 128, 4, 2, 2>());
+    case 3: return f(TileShape<128, 128, 2, 2, 2>());
+    case 4: return f(TileShape<96, 96, 2, 3, 3>());
+    default: return f(TileShape<64, 64, 2, 2, 3>());
+  }
+}
+inline double tile_us(const TileKind& k, bool split, int64_t tiles, int64_t pieces) {
+  const double many = (double)((tiles + 255) / 256) * k.busy[split];
+  return (double)pieces * (many > k.alone[split] ? many : k.alone[split]);
+}
+
 // Consecutive workgroups go round the 8 XCDs, each with an L2 of its own: this turns
 // a workgroup's number into one that is consecutive within an XCD, so that the
 // tiles an XCD has in flight share operand rows.

@@ -36,39 +36,32 @@ constexpr int kBlock = 256;
 constexpr int kUnitX = 12, kUnitA = 10;
 constexpr int kNormParts = 1024;  // most partial sums of a matrix
 
-// A product's tiles and slices by an estimate of its time (us): a piece of a tile
-// takes `alone` if a CU has one tile and `busy` a tile if it has several (512 x 512 x
-// 8192 bytes and 8192^2 outputs; one f16 number, two).  Slices mean that their sums
-// are written and read (5 TB/s) and a second kernel (4).
+// A product's tiles and slices by an estimate of its time: tile_us, and slices mean
+// that their sums are written and read (5 TB/s) and a second kernel (4 us).
 struct MmPlan {
-  int32_t side, slices, per;
+  int32_t kind, slices, per;
   int64_t bytes;
 };
-struct TileKind {
-  int32_t side;
-  double alone[2], busy[2];
-};
-constexpr TileKind kKinds[] = {{256, {1.38, 1.74}, {1.74, 2.21}}, {128, {0.57, 0.64}, {0.58, 0.61}},
-                               {64, {0.29, 0.32}, {0.18, 0.20}}};
 constexpr int64_t kMostPartBytes = 128 << 20;
 
-MmPlan plan_mm(int64_t m, int64_t n, int64_t pieces, int64_t batch, bool symmetric, bool sliceable, bool split) {
+MmPlan plan_mm(int64_t m, int64_t n, int64_t pieces, int64_t batch, bool symmetric, bool split) {
   MmPlan best{};
   double least = 1e30;
-  for (const TileKind& kind : kKinds) {
-    const int64_t tm = (m + kind.side - 1) / kind.side, tn = (n + kind.side - 1) / kind.side;
+  for (int t = 0; t < kTileKindCount; ++t) {
+    const TileKind& kind = kTileKinds[t];
+    if (symmetric && kind.tm != kind.tn) continue;
+    const int64_t tm = (m + kind.tm - 1) / kind.tm, tn = (n + kind.tn - 1) / kind.tn;
     const int64_t tiles = (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batch;
-    for (int64_t s = 1; s <= (sliceable ? 32 : 1) && s <= pieces; ++s) {
+    for (int64_t s = 1; s <= (symmetric ? 32 : 1) && s <= pieces; ++s) {
       const int64_t per = (pieces + s - 1) / s, used = (pieces + per - 1) / per;
       if (used != s) continue;
-      const int64_t bytes = s > 1 ? s * tiles * kind.side * kind.side * 4 : 0;
+      const int64_t bytes = s > 1 ? s * tiles * kind.tm * kind.tn * 4 : 0;
       if (bytes > kMostPartBytes) break;
-      const int64_t a_cu = (tiles * s + 255) / 256;
-      double us = per * std::max(kind.alone[split], a_cu * kind.busy[split]);
+      double us = tile_us(kind, split, tiles * s, per);
       if (s > 1) us += 4. + 2. * bytes / 5e6;
       if (us < least) {
         least = us;
-        best = {kind.side, (int32_t)s, (int32_t)per, bytes};
+        best = {t, (int32_t)s, (int32_t)per, bytes};
       }
     }
   }
@@ -102,9 +95,9 @@ Plan make_plan(const dfp_ortho_desc& d, bool split) {
   };
   const int64_t n = p.Rp * p.Cp * d.batch, s = p.rp * p.rp * d.batch;
   const int64_t per_piece = split ? 32 : 64;
-  p.mgram = plan_mm(p.rp, p.rp, (p.tall ? p.Rp : p.Cp) / per_piece, d.batch, true, true, split);
-  p.mpoly = plan_mm(p.rp, p.rp, p.rp / per_piece, d.batch, true, true, split);
-  p.mstep = plan_mm(p.Rp, p.Cp, p.rp / per_piece, d.batch, false, false, split);
+  p.mgram = plan_mm(p.rp, p.rp, (p.tall ? p.Rp : p.Cp) / per_piece, d.batch, true, split);
+  p.mpoly = plan_mm(p.rp, p.rp, p.rp / per_piece, d.batch, true, split);
+  p.mstep = plan_mm(p.Rp, p.Cp, p.rp / per_piece, d.batch, false, split);
   p.xlo = take(split ? 0 : n * 2);
   p.gram = take(n * p.e);
   p.step0 = take(n * p.e);
@@ -241,6 +234,12 @@ __global__ __launch_bounds__(kBlock) void k_pack(Source<T> s, int64_t R, int64_t
   const int64_t b = blockIdx.y;
   const int64_t ct = Cp / 64, r0 = blockIdx.x / ct * 64, c0 = blockIdx.x % ct * 64;
   const int cc = (threadIdx.x & 15) * 4;
+  double sums[kNormParts / kBlock];
+#pragma unroll
+  for (int i = 0; i < kNormParts / kBlock; ++i) {
+    const int32_t at = threadIdx.x + i * kBlock;
+    sums[i] = at < parts ? part[b * parts + at] : 0.;
+  }
   float u[4][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -248,8 +247,7 @@ __global__ __launch_bounds__(kBlock) void k_pack(Source<T> s, int64_t R, int64_t
     u[i][0] = u[i][1] = u[i][2] = u[i][3] = 0.f;
     if (r < R && c < C) direction<T, MUON>(s, (b * R + r) * C + c, C - c, u[i]);
   }
-  double sum = 0.;
-  for (int32_t i = threadIdx.x; i < parts; i += kBlock) sum += part[b * parts + i];
+  double sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = sum;
@@ -398,7 +396,7 @@ __device__ __forceinline__ void finish(const MmArgs& g, int64_t b, int64_t i0, i
     if (KIND == STEP && ONE) *(uint4*)(g.xlo + (b * g.m + i) * (int64_t)g.n + j) = pack8_low(v);
   }
   if (KIND == LAST || !mirror) return;
-  // (g.m is a multiple of 64: a wave's rows are all in or, from kRows = 64 on, all out)
+  // (g.m and g.n are multiples of 64: runs of eight are in or out as a whole)
 #pragma unroll
   for (int part = 0; part < (P == Prod::F16X2 ? 2 : 1); ++part) {
 #pragma unroll
@@ -412,7 +410,7 @@ __device__ __forceinline__ void finish(const MmArgs& g, int64_t b, int64_t i0, i
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int k = 0; k < kRows / 16; ++k) {
-      const int c = k * (512 / kRows) + lane / (kRows / 8), q = lane % (kRows / 8) * 8;
+      const int c = (k * 64 + lane) / (kRows / 8), q = (k * 64 + lane) % (kRows / 8) * 8;
       const uint4 d = *(const uint4*)(lds + c * kStride + q);
       if (j0 + c < g.n && i0 + q < g.m)
         *(uint4*)(g.colop + b * g.sc + (j0 + c) * g.ldc + op_off<P>(i0 + q) + part * 64) = d;
@@ -474,16 +472,24 @@ __global__ __launch_bounds__(64 * WM * WN) void k_sum(MmArgs g) {
   const int64_t stride = (int64_t)g.tiles * (TM * TN / 4);  // of a slice
   const mv4f* d = (const mv4f*)g.part + b * g.slices * stride + (int64_t)id * (TM * TN / 4) + threadIdx.x;
   float s[FM][8] = {};
-  for (int32_t k = 0; k < g.slices; ++k, d += stride) {
-    mv4f v[FM][2];
+  constexpr int U = FM > 2 ? 4 : 8;  // slices in flight
+  for (int32_t k = 0; k < g.slices; k += U) {
+    mv4f v[U][FM][2];
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) v[i][h] = d[((j + h) * FM + i) * Tile::kThreads];
+      for (int i = 0; i < FM; ++i)
 #pragma unroll
-    for (int i = 0; i < FM; ++i)
+        for (int h = 0; h < 2; ++h)
+          v[u][i][h] = d[min(k + u, g.slices - 1) * stride + ((j + h) * FM + i) * Tile::kThreads];
 #pragma unroll
-      for (int r = 0; r < 8; ++r) s[i][r] += v[i][r >> 2][r & 3];
+    for (int u = 0; u < U; ++u)
+      if (k + u < g.slices) {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+          for (int r = 0; r < 8; ++r) s[i][r] += v[u][i][r >> 2][r & 3];
+      }
   }
   const int wave = threadIdx.x >> 6;
   finish<P, KIND, 0, false, FM>(g, b, (int64_t)im * TM + (wave / WN) * (TM / WM),
@@ -492,32 +498,33 @@ __global__ __launch_bounds__(64 * WM * WN) void k_sum(MmArgs g) {
 
 template <Prod P, int KIND, int T, bool MUON>
 dfp_status launch_mm(int32_t id, const MmPlan& p, int32_t batch, MmArgs& g, hipStream_t st) {
-  g.tm = (uint32_t)((g.m + p.side - 1) / p.side);
-  g.tn = (uint32_t)((g.n + p.side - 1) / p.side);
+  const TileKind& kind = kTileKinds[p.kind];
+  g.tm = (uint32_t)((g.m + kind.tm - 1) / kind.tm);
+  g.tn = (uint32_t)((g.n + kind.tn - 1) / kind.tn);
   g.per = p.per;
   g.slices = p.slices;
   constexpr bool SYM = KIND == GRAM || KIND == POLY;
   g.tiles = SYM ? g.tm * (g.tm + 1) / 2 : g.tm * g.tn;
   const uint32_t wgs = g.tiles * (uint32_t)batch;
-  auto go = [&](auto side, auto wm, auto wn, auto s) -> dfp_status {
-    constexpr int D = decltype(side)::value, WM = decltype(wm)::value, WN = decltype(wn)::value;
-    constexpr int S = decltype(s)::value;
+  return with_tile(p.kind, [&](auto shape) -> dfp_status {
+    typedef decltype(shape) Q;
+    constexpr int TM = Q::TM, TN = Q::TN, WM = Q::WM, WN = Q::WN;
     const dim3 block(64 * WM * WN);
-    if constexpr (SYM) {
-      if (p.slices > 1) {
-        DFP_LAUNCH(id, (k_mm<P, KIND, T, MUON, true, D, D, WM, WN, S>), dim3(wgs * p.slices), block, 0, st, g);
-        DFP_LAUNCH(id, (k_sum<P, KIND, D, D, WM, WN>), dim3(g.tiles * (D / WN / 32), (unsigned)batch), block, 0,
-                   st, g);
-        return DFP_OK;
+    if constexpr (SYM && TM != TN) {
+      return DFP_ERR_PARAM;  // (no plan has it)
+    } else {
+      if constexpr (SYM) {
+        if (p.slices > 1) {
+          DFP_LAUNCH(id, (k_mm<P, KIND, T, MUON, true, TM, TN, WM, WN, Q::S>), dim3(wgs * p.slices), block, 0, st, g);
+          DFP_LAUNCH(id, (k_sum<P, KIND, TM, TN, WM, WN>), dim3(g.tiles * (TN / WN / 32), (unsigned)batch), block, 0,
+                     st, g);
+          return DFP_OK;
+        }
       }
+      DFP_LAUNCH(id, (k_mm<P, KIND, T, MUON, false, TM, TN, WM, WN, Q::S>), dim3(wgs), block, 0, st, g);
+      return DFP_OK;
     }
-    DFP_LAUNCH(id, (k_mm<P, KIND, T, MUON, false, D, D, WM, WN, S>), dim3(wgs), block, 0, st, g);
-    return DFP_OK;
-  };
-  typedef std::integral_constant<int, 2> Two;
-  if (p.side == 256) return go(std::integral_constant<int, 256>(), std::integral_constant<int, 4>(), Two(), Two());
-  if (p.side == 128) return go(std::integral_constant<int, 128>(), Two(), Two(), Two());
-  return go(std::integral_constant<int, 64>(), Two(), Two(), std::integral_constant<int, 3>());
+  });
 }
 
 // Largest unit of a I + B that keeps it at 32768 or less for |X| <= sqrt(2).
@@ -541,7 +548,7 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
   double* part = (double*)(base + p.norm);
   const unsigned nb = (unsigned)d.batch;
   const int64_t n = p.R * p.C;
-  const int32_t parts = (int32_t)std::min<int64_t>(kNormParts, (n + kBlock * 4 - 1) / (kBlock * 4));
+  const int32_t parts = (int32_t)std::min<int64_t>(n < (1 << 23) ? kBlock : kNormParts, (n + kBlock * 4 - 1) / (kBlock * 4));
   DFP_LAUNCH(K_ORTHO_NORM, (k_norm<T, MUON>), dim3((unsigned)parts, nb), dim3(kBlock), 0, st, src, n, part);
   // gram: the longer side contiguous
   uint8_t* rowop = p.tall ? step[0] : gram;
@@ -603,7 +610,7 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
     if (s + 1 < d.steps)
       rc = launch_mm<P, STEP, 0, false>(K_ORTHO_STEP, p.mstep, d.batch, g, st);
     else
-      rc = launch_mm<P, LAST, T, MUON>(K_ORTHO_STEP, p.mstep, d.batch, g, st);
+      rc = launch_mm<P, LAST, MUON ? DFP_F32 : T, MUON>(K_ORTHO_STEP, p.mstep, d.batch, g, st);
     if (rc != DFP_OK) return rc;
   }
   return DFP_OK;
