@@ -44,7 +44,7 @@ struct MmPlan {
 };
 constexpr int64_t kMostPartBytes = 128 << 20;
 
-MmPlan plan_mm(int64_t m, int64_t n, int64_t pieces, int64_t batch, bool symmetric, bool split) {
+MmPlan plan_mm(int64_t m, int64_t n, int64_t pieces, int64_t batch, bool symmetric, bool sliceable, bool split) {
   MmPlan best{};
   double least = 1e30;
   for (int t = 0; t < kTileKindCount; ++t) {
@@ -52,7 +52,7 @@ MmPlan plan_mm(int64_t m, int64_t n, int64_t pieces, int64_t batch, bool symmetr
     if (symmetric && kind.tm != kind.tn) continue;
     const int64_t tm = (m + kind.tm - 1) / kind.tm, tn = (n + kind.tn - 1) / kind.tn;
     const int64_t tiles = (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batch;
-    for (int64_t s = 1; s <= (symmetric ? 32 : 1) && s <= pieces; ++s) {
+    for (int64_t s = 1; s <= (sliceable ? 32 : 1) && s <= pieces; ++s) {
       const int64_t per = (pieces + s - 1) / s, used = (pieces + per - 1) / per;
       if (used != s) continue;
       const int64_t bytes = s > 1 ? s * tiles * kind.tm * kind.tn * 4 : 0;
@@ -95,9 +95,10 @@ Plan make_plan(const dfp_ortho_desc& d, bool split) {
   };
   const int64_t n = p.Rp * p.Cp * d.batch, s = p.rp * p.rp * d.batch;
   const int64_t per_piece = split ? 32 : 64;
-  p.mgram = plan_mm(p.rp, p.rp, (p.tall ? p.Rp : p.Cp) / per_piece, d.batch, true, split);
-  p.mpoly = plan_mm(p.rp, p.rp, p.rp / per_piece, d.batch, true, split);
-  p.mstep = plan_mm(p.Rp, p.Cp, p.rp / per_piece, d.batch, false, split);
+  // (only the Gram product has reductions longer than its sides)
+  p.mgram = plan_mm(p.rp, p.rp, (p.tall ? p.Rp : p.Cp) / per_piece, d.batch, true, true, split);
+  p.mpoly = plan_mm(p.rp, p.rp, p.rp / per_piece, d.batch, true, false, split);
+  p.mstep = plan_mm(p.Rp, p.Cp, p.rp / per_piece, d.batch, false, false, split);
   p.xlo = take(split ? 0 : n * 2);
   p.gram = take(n * p.e);
   p.step0 = take(n * p.e);
@@ -106,7 +107,7 @@ Plan make_plan(const dfp_ortho_desc& d, bool split) {
   p.bb = take(s * p.e);
   p.diag = take(split ? 0 : p.rp * d.batch * 4);
   p.norm = take((int64_t)kNormParts * d.batch * 8);
-  p.slices = take(std::max(p.mgram.bytes, p.mpoly.bytes));
+  p.slices = take(p.mgram.bytes);
   p.bytes = at;
   return p;
 }
@@ -295,7 +296,7 @@ struct MmArgs {
   float* part;             // slices: [batch][slice][tile][quad][thread] of four sums
   float unit;              // of the sum
   // outputs
-  uint8_t *rowop, *colop;  // operand and (GRAM / POLY: the same) its transpose
+  uint8_t *rowop, *colop;  // operand and (GRAM, POLY: the same) its transpose
   int64_t ldr, ldc, sr, sc;
   const uint8_t* old;      // POLY: A; STEP, LAST of one part: X's high part; in rowop's layout
   float* diag;             // one part: POLY writes, STEP reads, [rp] a matrix
@@ -460,7 +461,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_mm(MmArgs g) {
 
 // The slices of a tile added up in their order, then as above: workgroups of a tile's
 // threads by one pair of fragment columns.
-template <Prod P, int KIND, int TM, int TN, int WM, int WN>
+template <Prod P, int TM, int TN, int WM, int WN>
 __global__ __launch_bounds__(64 * WM * WN) void k_sum(MmArgs g) {
   typedef MmaTile<P, TM, TN, WM, WN, 2> Tile;
   constexpr int FM = Tile::FM, FN = Tile::FN;
@@ -468,7 +469,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_sum(MmArgs g) {
   const int64_t b = blockIdx.y;
   const uint32_t id = blockIdx.x / (FN / 2), j = blockIdx.x % (FN / 2) * 2;
   uint32_t im, in;
-  mm_tile<KIND>(g, id, &im, &in);
+  mm_tile<GRAM>(g, id, &im, &in);
   const int64_t stride = (int64_t)g.tiles * (TM * TN / 4);  // of a slice
   const mv4f* d = (const mv4f*)g.part + b * g.slices * stride + (int64_t)id * (TM * TN / 4) + threadIdx.x;
   float s[FM][8] = {};
@@ -492,7 +493,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_sum(MmArgs g) {
       }
   }
   const int wave = threadIdx.x >> 6;
-  finish<P, KIND, 0, false, FM>(g, b, (int64_t)im * TM + (wave / WN) * (TM / WM),
+  finish<P, GRAM, 0, false, FM>(g, b, (int64_t)im * TM + (wave / WN) * (TM / WM),
                                 (int64_t)in * TN + (wave % WN) * (TN / WN) + j * 16, im != in, lds[wave], s);
 }
 
@@ -513,10 +514,10 @@ dfp_status launch_mm(int32_t id, const MmPlan& p, int32_t batch, MmArgs& g, hipS
     if constexpr (SYM && TM != TN) {
       return DFP_ERR_PARAM;  // (no plan has it)
     } else {
-      if constexpr (SYM) {
+      if constexpr (KIND == GRAM) {
         if (p.slices > 1) {
           DFP_LAUNCH(id, (k_mm<P, KIND, T, MUON, true, TM, TN, WM, WN, Q::S>), dim3(wgs * p.slices), block, 0, st, g);
-          DFP_LAUNCH(id, (k_sum<P, KIND, TM, TN, WM, WN>), dim3(g.tiles * (TN / WN / 32), (unsigned)batch), block, 0,
+          DFP_LAUNCH(id, (k_sum<P, TM, TN, WM, WN>), dim3(g.tiles * (TN / WN / 32), (unsigned)batch), block, 0,
                      st, g);
           return DFP_OK;
         }

@@ -1,0 +1,118 @@
+"""Every tile and way of slicing that the products' estimates choose, at sizes that
+reach each of them, against 64-bit products on the GPU (integers are exact there).
+Tolerances as in test_gpu_linear_i8.py and test_gpu_ortho.py."""
+import numpy as np
+import pytest
+import torch
+
+import linear_ref as ref
+from gpu_helpers import DEV, note
+from paper_1802_00930_amd import dfp
+
+pytestmark = pytest.mark.gpu
+
+# tile, slices: m, n, k
+PRODUCTS = [
+    (66, 16892, 100),      # 96 x 96
+    (1500, 1500, 500),
+    (134, 32975, 200),     # 192 x 192
+    (3000, 3000, 257),
+    (49252, 135, 40),      # 256 x 256
+    (4000, 4090, 300),
+    (33709, 70, 129),      # 192 x 128
+    (3000, 2000, 1000),
+    (68, 26785, 300),      # 128 x 128
+    (2000, 2000, 200),
+    (1100, 1500, 700),     # 64 x 64
+    (65, 3, 1965),         # the same, 16 slices
+    (200, 300, 30000),
+    (69, 2051, 3667),      # 96 x 96, 8
+    (73, 6667, 6926),      # 128 x 128, 4
+    (3258, 67, 15308),     # 192 x 128, 15
+    (3248, 148, 22892),    # 192 x 192, 15
+    (3597, 148, 75337),    # 256 x 256, 16
+    (64, 1, 1),            # rows of a batch
+    (40, 9000, 3000),
+    (24, 5000, 8192),
+]
+
+
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("m,n,k", PRODUCTS)
+def test_product(m, n, k, t):
+    note("tiles %dx%dx%d %s" % (m, n, k, t))
+    g = torch.Generator(device=DEV)
+    g.manual_seed(m + n + k)
+    a, b = (torch.zeros(r, ref.ld(k), dtype=torch.int8, device=DEV) for r in (m, n))
+    for x in (a, b):
+        x[:, :k] = torch.randint(-127, 128, (x.shape[0], k), generator=g, device=DEV, dtype=torch.int8)
+    sa, sb = (torch.rand(r, generator=g, device=DEV) * 2.0 ** -6 for r in (m, n))
+    bias = torch.randn(n, generator=g, device=DEV)
+    d = dfp.make_linear_desc(m, n, k, t)
+    raw = torch.full((m * n + 256,), 77, dtype=t, device=DEV)
+    ws = torch.full((dfp.linear_i8_workspace_bytes(d),), 0x81, dtype=torch.uint8, device=DEV)
+    out = raw[:m * n].view(m, n)
+    dfp.dfp_gemm_i8(d, a, sa, b, sb, out, bias=bias, workspace=ws)
+    y = torch.mm(a.double(), b.double().t()) * sa.double()[:, None] * sb.double()[None, :]
+    size = y.abs() + bias.double().abs()[None, :]
+    y = y + bias.double()[None, :]
+    half = 2.0 ** -24 if t is torch.float32 else 2.0 ** -8
+    tol = 4 * 2.0 ** -24 * (size + y.abs()) + half * 1.0001 * y.abs()
+    assert bool(((out.double() - y).abs() <= tol).all())
+    assert bool((raw[m * n:] == 77).all())
+
+
+# Gram, polynomial and step tiles; one f16 number (BF16) or two
+ORTHO = [
+    ("bf16", 9, 1175, 924),    # 96 x 96
+    ("bf16", 1, 2641, 1146),   # Gram 96 x 96 in slices
+    ("bf16", 9, 875, 977),     # 128 x 128
+    ("bf16", 1, 7154, 1009),   # Gram 128 x 128 in slices
+    ("bf16", 9, 1154, 1109),   # 192 x 192
+    ("bf16", 1, 1312, 14953),  # Gram 192 x 192 in slices
+    ("bf16", 9, 1550, 1928),   # 256 x 256
+    ("bf16", 4, 996, 10316),   # Gram 256 x 256 in slices
+    ("bf16", 9, 134, 1234),    # step 96 x 96
+    ("bf16", 9, 3896, 67),     # step 192 x 128
+    ("bf16", 4, 131, 8562),    # step 192 x 192
+    ("bf16", 9, 6071, 144),    # step 256 x 256
+    ("f32", 9, 1038, 917),     # 96 x 96
+    ("f32", 4, 531, 1469),     # Gram 96 x 96 in slices
+    ("f32", 9, 819, 921),      # 128 x 128
+    ("f32", 1, 849, 4228),     # Gram 128 x 128 in slices
+    ("f32", 9, 1807, 1303),    # 192 x 192
+    ("f32", 1, 9751, 1286),    # Gram 192 x 192 in slices
+    ("f32", 9, 1693, 1632),    # 256 x 256
+    ("f32", 1, 1995, 7899),    # Gram 256 x 256 in slices
+    ("f32", 1, 11162, 130),    # step 96 x 96
+    ("f32", 9, 69, 3646),      # step 192 x 128
+    ("f32", 4, 10127, 129),    # step 192 x 192
+    ("f32", 4, 140, 15184),    # step 256 x 256
+]
+COEF = (3.4445, -4.7750, 2.0315)
+
+
+@pytest.mark.parametrize("t,b,r,c", ORTHO)
+def test_orthogonalize(t, b, r, c):
+    note("ortho tiles %s %dx%dx%d" % (t, b, r, c))
+    dt = torch.float32 if t == "f32" else torch.bfloat16
+    g = torch.Generator(device=DEV)
+    g.manual_seed(r + c)
+    x = (torch.randn(b, r, c, generator=g, device=DEV) * torch.exp(0.5 * torch.randn(b, r, 1, generator=g, device=DEV)))
+    x = (1e-3 * x).to(dt)
+    d = dfp.make_ortho_desc(b, r, c, dt)
+    raw = torch.full((b * r * c + 256,), 7, dtype=dt, device=DEV)
+    out = raw[:b * r * c].view(b, r, c)
+    ws = torch.full((dfp.ortho_workspace_bytes(d),), 0xff, dtype=torch.uint8, device=DEV)
+    dfp.dfp_orthogonalize(d, x, out, workspace=ws)
+    for i in range(b):
+        u = x[i].double()
+        u = u.t().contiguous() if r > c else u
+        u = u / (torch.linalg.vector_norm(u) + 1e-7)
+        for _ in range(5):
+            a = torch.mm(u, u.t().contiguous())
+            u = COEF[0] * u + torch.mm(COEF[1] * a + COEF[2] * torch.mm(a, a), u)
+        u = u.t() if r > c else u
+        off = float(torch.linalg.vector_norm(out[i].double() - u) / torch.linalg.vector_norm(u))
+        assert np.isfinite(off) and off <= (2e-4 if t == "f32" else 3e-3), (i, off)
+    assert bool((raw[b * r * c:] == 7).all())
