@@ -46,9 +46,10 @@ __device__ __forceinline__ void store_quad(const I8Args& g, int64_t i, int64_t j
 }
 
 // SLICED: the tiles of every slice in turn, their sums to g.part.
-template <int T, bool SLICED, int TM, int TN, int WM, int WN, int S>
-__global__ __launch_bounds__(64 * WM * WN, 2) void k_tiles(I8Args g) {
-  typedef MmaTile<Prod::I8, TM, TN, WM, WN, S> Tile;
+template <int T, bool SLICED, class Q>
+__global__ __launch_bounds__(Q::kThreads, 2) void k_tiles(I8Args g) {
+  typedef typename Q::template Tile<Prod::I8> Tile;
+  constexpr int TM = Q::TM, TN = Q::TN, WM = Q::WM, WN = Q::WN;
   const uint32_t id = xcd_order(blockIdx.x, gridDim.x), tiles = g.tm * g.tn, slice = SLICED ? id / tiles : 0;
   uint32_t im, in;
   tile_of(id - slice * tiles, g.tm, g.tn, 8, &im, &in);
@@ -59,8 +60,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_tiles(I8Args g) {
   // they cost 2 us of memory's latency (1500 x 2048 x 128: 6.1 us in all).
   __shared__ __align__(16) float fa[TM], fb[TN], fbias[TN];
   if (!SLICED) {
-    for (int t = threadIdx.x; t < TM; t += 64 * WM * WN) fa[t] = g.sa[min(i0 + t, (int64_t)g.m - 1)];
-    for (int t = threadIdx.x; t < TN; t += 64 * WM * WN) {
+    for (int t = threadIdx.x; t < TM; t += Q::kThreads) fa[t] = g.sa[min(i0 + t, (int64_t)g.m - 1)];
+    for (int t = threadIdx.x; t < TN; t += Q::kThreads) {
       const int64_t c = min(j0 + t, (int64_t)g.n - 1);
       fb[t] = g.sb ? g.sb[c] : 1.f;
       fbias[t] = g.bias ? g.bias[c] : 0.f;
@@ -69,6 +70,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_tiles(I8Args g) {
   mv4i acc[Tile::FM][Tile::FN];
   Tile::run(g.a + i0 * g.ld + (int64_t)p0 * kPiece, g.ld, (int32_t)(g.m - i0),
             g.b + j0 * g.ld + (int64_t)p0 * kPiece, g.ld, (int32_t)(g.n - j0), pieces, acc);
+  if (threadIdx.x >= Tile::kThreads) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t i1 = i0 + (wave / WN) * (TM / WM) + (lane & 15);
   const int64_t j1 = j0 + (wave % WN) * (TN / WN) + (lane >> 4) * 8;
@@ -347,8 +349,8 @@ dfp_status launch_gemm_i8(int32_t m, int32_t n, int32_t k, const int8_t* a, cons
       constexpr int TT = SL ? DFP_F32 : T;
       return with_tile(p.kind, [&](auto shape) -> dfp_status {
         typedef decltype(shape) Q;
-        DFP_LAUNCH(K_I8_GEMM, (k_tiles<TT, SL, Q::TM, Q::TN, Q::WM, Q::WN, Q::S>),
-                   dim3(g.tm * g.tn * (unsigned)p.slices), dim3(64 * Q::WM * Q::WN), 0, st, g);
+        DFP_LAUNCH(K_I8_GEMM, (k_tiles<TT, SL, Q>), dim3(g.tm * g.tn * (unsigned)p.slices), dim3(Q::kThreads), 0, st,
+                   g);
         return DFP_OK;
       });
     };

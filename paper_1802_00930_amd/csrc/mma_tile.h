@@ -65,10 +65,15 @@ typedef __attribute__((address_space(3))) void* mma_lds_t;
 // the cycles, at 2.07 GHz).  Staging through registers reaches 2240, 1110 and 1210,
 // 128 x 128 outputs a wave (one wave a SIMD) 1840; two groups of waves that
 // take turns between reads and MFMAs, four barriers a piece, 2070.
-template <Prod P, int TM, int TN, int WM, int WN, int S>
+//
+// KG > 1: as many groups of WM x WN waves take the pieces in turn, each with a ring of
+// its own, and group 0 ends with the sums of all: for a CU that has one tile, where a
+// group spends much of its time waiting (64 x 64, 512 x 512 x 8192 bytes: 20.6 us, two
+// groups 15.9, three 15.5: 28 bytes a clock then come from L2 to the CU).
+template <Prod P, int TM, int TN, int WM, int WN, int S, int KG>
 struct MmaTile {
   typedef typename MmaTypes<P>::acc_t acc_t;
-  static constexpr int kThreads = 64 * WM * WN;
+  static constexpr int kThreads = 64 * WM * WN;  // of a group
   static constexpr int FM = TM / WM / 16, FN = TN / WN / 16;
   static constexpr int kLoadsA = TM * 8 / kThreads, kLoadsB = TN * 8 / kThreads;  // 16-byte quads of a thread
   static constexpr int kStage = (TM + TN) * kPiece;
@@ -86,7 +91,7 @@ struct MmaTile {
   }
   template <int I>
   static __device__ __forceinline__ uint8_t* stage() {
-    __shared__ __align__(16) uint8_t s[kStage];
+    __shared__ __align__(16) uint8_t s[KG * kStage];
     return s;
   }
 
@@ -95,7 +100,8 @@ struct MmaTile {
   // rows span less than 2^31 bytes.
   static __device__ __forceinline__ void run(const uint8_t* a, int64_t lda, int32_t na, const uint8_t* b, int64_t ldb,
                                              int32_t nb, int32_t pieces, acc_t (&acc)[FM][FN]) {
-    const int t = threadIdx.x;
+    const int kg = KG > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads) : 0;
+    const int t = threadIdx.x - kg * kThreads;
     const int lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int wm = wave / WN, wn = wave % WN;
     int32_t offa[kLoadsA], offb[kLoadsB];
@@ -118,7 +124,10 @@ struct MmaTile {
 #pragma unroll
       for (int j = 0; j < FN; ++j) acc[i][j] = acc_t{0, 0, 0, 0};
 
-    auto fetch = [&](int32_t p, uint8_t* s) {
+    // (step q: piece q KG + kg)
+    auto fetch = [&](int32_t q, uint8_t* base) {
+      uint8_t* s = base + kg * kStage;
+      const int32_t p = min(q * KG + kg, pieces - 1);
 #pragma unroll
       for (int i = 0; i < kLoadsA; ++i)
         __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (mma_lds_t)(s + (i * kThreads + wave * 64) * 16), 16, offa[i],
@@ -129,7 +138,8 @@ struct MmaTile {
                                                  16, offb[i], p * kPiece, 0, 0);
       __builtin_amdgcn_sched_barrier(0);  // not behind the reads of the other stage
     };
-    auto compute = [&](const uint8_t* s) {
+    auto compute = [&](const uint8_t* base) {
+      const uint8_t* s = base + kg * kStage;
       mv4i qa[2][FM], qb[2][FN];
       // quads g and 4 + g of every row: the second is the first with bit 6 turned
       auto read_a = [&](int h) {
@@ -171,18 +181,39 @@ struct MmaTile {
       // done reading q - 1.  (As assembly: the compiler's barrier would wait for
       // every load in flight.)
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((S - 2) * (kLoadsA + kLoadsB)) : "memory");
-      fetch(min(q + S - 1, pieces - 1), stage<(I + S - 1) % S>());
-      compute(stage<I>());
+      fetch(q + S - 1, stage<(I + S - 1) % S>());
+      if (KG == 1 || q * KG + kg < pieces) compute(stage<I>());
     };
     for_stages([&](auto at) {
       constexpr int I = decltype(at)::value;
-      if constexpr (I < S - 1) fetch(min(I, pieces - 1), stage<I>());
+      if constexpr (I < S - 1) fetch(I, stage<I>());
     });
-    for (int32_t q = 0; q < pieces; q += S)
+    const int32_t steps = (pieces + KG - 1) / KG;
+    for (int32_t q = 0; q < steps; q += S)
       for_stages([&](auto at) {
-        if (q + decltype(at)::value < pieces) step(q + decltype(at)::value, at);
+        if (q + decltype(at)::value < steps) step(q + decltype(at)::value, at);
       });
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if constexpr (KG > 1) {
+      static_assert((KG - 1) * FM * FN * 16 * kThreads <= KG * kStage, "the groups' sums in a stage");
+      acc_t* m = (acc_t*)stage<0>();
+      __syncthreads();
+      if (kg > 0) {
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+          for (int j = 0; j < FN; ++j) m[((kg - 1) * FM * FN + i * FN + j) * kThreads + t] = acc[i][j];
+      }
+      __syncthreads();
+      if (kg == 0) {
+#pragma unroll
+        for (int k = 0; k < KG - 1; ++k)
+#pragma unroll
+          for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] += m[(k * FM * FN + i * FN + j) * kThreads + t];
+      }
+    }
   }
 };
 
@@ -191,20 +222,24 @@ struct MmaTile {
 // 8192^2 x 8192).  Outputs of a tile per time fall with its side, but a product takes
 // as long as the CU with the most tiles, and 256 CUs are filled in steps: 3008 x 3008
 // x 4096 takes 63.6, 42.7, 46.8, 55.0, 59.1 and 65.3 with these.
-template <int TM_, int TN_, int WM_, int WN_, int S_>
+template <int TM_, int TN_, int WM_, int WN_, int S_, int KG_ = 1>
 struct TileShape {
-  static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, S = S_;
+  static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, S = S_, KG = KG_;
+  static constexpr int kThreads = 64 * WM * WN * KG;  // of the workgroup
+  template <Prod P>
+  using Tile = MmaTile<P, TM, TN, WM, WN, S, KG>;
 };
 struct TileKind {
   int32_t tm, tn;
-  double alone[2], busy[2];
+  double alone[2], busy[2], once;  // once: whatever the reduction (the groups' sums)
 };
 constexpr TileKind kTileKinds[] = {
-    {256, 256, {1.38, 1.74}, {1.78, 2.22}}, {192, 192, {0.85, 1.05}, {1.14, 1.42}},
-    {192, 128, {0.67, 0.75}, {0.67, 0.88}}, {128, 128, {0.58, 0.64}, {0.58, 0.62}},
-    {96, 96, {0.39, 0.44}, {0.39, 0.46}},   {64, 64, {0.31, 0.33}, {0.18, 0.20}},
+    {256, 256, {1.38, 1.74}, {1.78, 2.22}, 0.}, {192, 192, {0.85, 1.05}, {1.14, 1.42}, 0.},
+    {192, 128, {0.67, 0.75}, {0.67, 0.88}, 0.}, {128, 128, {0.58, 0.64}, {0.58, 0.62}, 0.},
+    {96, 96, {0.39, 0.44}, {0.39, 0.46}, 0.},   {64, 64, {0.31, 0.33}, {0.18, 0.20}, 0.},
+    {64, 64, {0.24, 0.26}, {0.24, 0.26}, 0.5},  // two groups
 };
-constexpr int kTileKindCount = 6;
+constexpr int kTileKindCount = 7;
 template <class F>
 dfp_status with_tile(int32_t kind, F f) {
   switch (kind) {
@@ -213,12 +248,13 @@ dfp_status with_tile(int32_t kind, F f) {
     case 2: return f(TileShape<192, 128, 4, 2, 2>());
     case 3: return f(TileShape<128, 128, 2, 2, 2>());
     case 4: return f(TileShape<96, 96, 2, 3, 3>());
-    default: return f(TileShape<64, 64, 2, 2, 3>());
+    case 5: return f(TileShape<64, 64, 2, 2, 3>());
+    default: return f(TileShape<64, 64, 2, 2, 3, 2>());
   }
 }
 inline double tile_us(const TileKind& k, bool split, int64_t tiles, int64_t pieces) {
   const double many = (double)((tiles + 255) / 256) * k.busy[split];
-  return (double)pieces * (many > k.alone[split] ? many : k.alone[split]);
+  return (double)pieces * (many > k.alone[split] ? many : k.alone[split]) + k.once;
 }
 
 // Consecutive workgroups go round the 8 XCDs, each with an L2 of its own: this turns

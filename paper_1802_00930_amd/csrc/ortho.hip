@@ -420,9 +420,10 @@ __device__ __forceinline__ void finish(const MmArgs& g, int64_t b, int64_t i0, i
   }
 }
 
-template <Prod P, int KIND, int T, bool MUON, bool SLICED, int TM, int TN, int WM, int WN, int S>
-__global__ __launch_bounds__(64 * WM * WN, 2) void k_mm(MmArgs g) {
-  typedef MmaTile<P, TM, TN, WM, WN, S> Tile;
+template <Prod P, int KIND, int T, bool MUON, bool SLICED, class Q>
+__global__ __launch_bounds__(Q::kThreads, 2) void k_mm(MmArgs g) {
+  typedef typename Q::template Tile<P> Tile;
+  constexpr int TM = Q::TM, TN = Q::TN, WM = Q::WM, WN = Q::WN;
   // matrices, their slices and those' tiles in order: an XCD's workgroups read few rows
   // (12 of 512 x 512 dealt out one by one: every XCD reads every matrix)
   const uint32_t id = xcd_order(blockIdx.x, gridDim.x), sl = id / g.tiles, tile = id - sl * g.tiles;
@@ -435,6 +436,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_mm(MmArgs g) {
   mv4f acc[Tile::FM][Tile::FN];
   Tile::run(g.a + b * g.sa + i0 * g.lda + at, g.lda, (int32_t)(g.m - i0), g.b + b * g.sb + j0 * g.ldb + at, g.ldb,
             (int32_t)(g.n - j0), pieces, acc);
+  if (!SLICED) __syncthreads();  // all waves are done with the stages
+  if (threadIdx.x >= Tile::kThreads) return;
   if (SLICED) {
     mv4f* d = (mv4f*)g.part + (int64_t)id * (TM * TN / 4) + threadIdx.x;
 #pragma unroll
@@ -444,7 +447,6 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_mm(MmArgs g) {
     return;
   }
   const int wave = threadIdx.x >> 6;
-  __syncthreads();  // all waves are done with the stages
   uint16_t* lds = (uint16_t*)(Tile::template stage<0>() + wave * (Tile::kStage / (WM * WN)));
   static_assert(32 * (16 * Tile::FM + 8) * 2 <= Tile::kStage / (WM * WN), "a wave's part of a stage");
 #pragma unroll
@@ -461,9 +463,10 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void k_mm(MmArgs g) {
 
 // The slices of a tile added up in their order, then as above: workgroups of a tile's
 // threads by one pair of fragment columns.
-template <Prod P, int TM, int TN, int WM, int WN>
-__global__ __launch_bounds__(64 * WM * WN) void k_sum(MmArgs g) {
-  typedef MmaTile<P, TM, TN, WM, WN, 2> Tile;
+template <Prod P, class Q>
+__global__ __launch_bounds__(64 * Q::WM * Q::WN) void k_sum(MmArgs g) {
+  typedef typename Q::template Tile<P> Tile;
+  constexpr int TM = Q::TM, TN = Q::TN, WM = Q::WM, WN = Q::WN;
   constexpr int FM = Tile::FM, FN = Tile::FN;
   __shared__ __align__(16) uint16_t lds[WM * WN][32 * (16 * FM + 8)];
   const int64_t b = blockIdx.y;
@@ -509,20 +512,18 @@ dfp_status launch_mm(int32_t id, const MmPlan& p, int32_t batch, MmArgs& g, hipS
   const uint32_t wgs = g.tiles * (uint32_t)batch;
   return with_tile(p.kind, [&](auto shape) -> dfp_status {
     typedef decltype(shape) Q;
-    constexpr int TM = Q::TM, TN = Q::TN, WM = Q::WM, WN = Q::WN;
-    const dim3 block(64 * WM * WN);
-    if constexpr (SYM && TM != TN) {
+    if constexpr (SYM && Q::TM != Q::TN) {
       return DFP_ERR_PARAM;  // (no plan has it)
     } else {
       if constexpr (KIND == GRAM) {
         if (p.slices > 1) {
-          DFP_LAUNCH(id, (k_mm<P, KIND, T, MUON, true, TM, TN, WM, WN, Q::S>), dim3(wgs * p.slices), block, 0, st, g);
-          DFP_LAUNCH(id, (k_sum<P, TM, TN, WM, WN>), dim3(g.tiles * (TN / WN / 32), (unsigned)batch), block, 0,
-                     st, g);
+          DFP_LAUNCH(id, (k_mm<P, KIND, T, MUON, true, Q>), dim3(wgs * p.slices), dim3(Q::kThreads), 0, st, g);
+          DFP_LAUNCH(id, (k_sum<P, Q>), dim3(g.tiles * (Q::TN / Q::WN / 32), (unsigned)batch),
+                     dim3(64 * Q::WM * Q::WN), 0, st, g);
           return DFP_OK;
         }
       }
-      DFP_LAUNCH(id, (k_mm<P, KIND, T, MUON, false, TM, TN, WM, WN, Q::S>), dim3(wgs), block, 0, st, g);
+      DFP_LAUNCH(id, (k_mm<P, KIND, T, MUON, false, Q>), dim3(wgs), dim3(Q::kThreads), 0, st, g);
       return DFP_OK;
     }
   });
