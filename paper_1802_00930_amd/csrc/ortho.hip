@@ -10,13 +10,13 @@
 // to 64 with zeros, which every step keeps zero.
 //
 // A and B are symmetric: only tiles on and above the diagonal are computed and each
-// is stored twice.  The diagonal of a I + B holds the largest entries of its rows: in
-// an operand of one f16 number it would be off by most, so it stays out of that and
-// joins in FP32, X = (a + B_ii) X + B' X; an operand of two takes it in, X = (a I + B) X,
-// and the step need not read X again.
+// is stored twice.  a X joins in FP32 (with a in B's operand, where it would be off by
+// 2^-23, the result is three times as far off for matrices of strong directions above
+// weak ones).  In an operand of one f16 number B's diagonal, the largest entries of its
+// rows, would be off by most: it stays out and joins too, X = (a + B_ii) X + B' X.
 //
-// Units: X in 2^-12, A in 2^-10, B in 2^-sb so that |a I + b A + c A A| <= 32768 in it
-// for singular values up to sqrt(2).
+// Units: X in 2^-12, A in 2^-10, B in 2^-sb so that |b A + c A A| <= 32768 in it for
+// singular values up to sqrt(2).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -298,7 +298,7 @@ struct MmArgs {
   // outputs
   uint8_t *rowop, *colop;  // operand and (GRAM, POLY: the same) its transpose
   int64_t ldr, ldc, sr, sc;
-  const uint8_t* old;      // POLY: A; STEP, LAST of one part: X's high part; in rowop's layout
+  const uint8_t* old;      // POLY: A; STEP, LAST: X (its high part); in rowop's layout
   float* diag;             // one part: POLY writes, STEP reads, [rp] a matrix
   float cb, cc, ca;        // coefficients
   float uout;              // unit of the operands written
@@ -342,11 +342,11 @@ __device__ __forceinline__ void finish(const MmArgs& g, int64_t b, int64_t i0, i
     hi[fi] = lo[fi] = make_uint4(0, 0, 0, 0);
     dg[fi] = 0.f;
     if (i >= g.m || !in_n) continue;
-    if (KIND == POLY || (XSTEP && ONE)) {
+    if (KIND == POLY || XSTEP) {
       const uint4* d = (const uint4*)(g.old + b * g.sr + i * g.ldr + op_off<P>(j));
       hi[fi] = d[0];
-      if (KIND == POLY && !ONE) lo[fi] = d[4];
-      if (XSTEP) lo[fi] = *(const uint4*)(g.xlo + (b * g.m + i) * (int64_t)g.n + j);
+      if (!ONE) lo[fi] = d[4];
+      if (XSTEP && ONE) lo[fi] = *(const uint4*)(g.xlo + (b * g.m + i) * (int64_t)g.n + j);
     }
     if (XSTEP && ONE && !g.diag_cols) dg[fi] = g.diag[b * g.rp + i];
     if (KIND == LAST && MUON && i < g.R && j < g.C) load_n<DFP_F32, 8>(g.w + (b * g.R + i) * g.C + j, g.C - j, w[fi]);
@@ -361,23 +361,21 @@ __device__ __forceinline__ void finish(const MmArgs& g, int64_t b, int64_t i0, i
 #pragma unroll
     for (int r = 0; r < 8; ++r) v[r] *= g.unit;
     float x[8];
-    if (KIND == POLY || (XSTEP && ONE)) unpack8(hi[fi], lo[fi], x);
+    if (KIND == POLY || XSTEP) unpack8(hi[fi], lo[fi], x);
     if (KIND == POLY) {
 #pragma unroll
       for (int r = 0; r < 8; ++r) {
         v[r] = fmaf(g.cc, v[r], g.cb * (x[r] * (1.f / (1 << kUnitA))));
-        if (i == j + r) {
-          v[r] += g.ca;
-          if (ONE) {
-            g.diag[b * g.rp + i] = v[r];
-            v[r] = 0.f;
-          }
+        if (ONE && i == j + r) {
+          g.diag[b * g.rp + i] = g.ca + v[r];
+          v[r] = 0.f;
         }
       }
     }
-    if (XSTEP && ONE) {
+    if (XSTEP) {
 #pragma unroll
-      for (int r = 0; r < 8; ++r) v[r] = fmaf(g.diag_cols ? dc[r] : dg[fi], x[r] * (1.f / (1 << kUnitX)), v[r]);
+      for (int r = 0; r < 8; ++r)
+        v[r] = fmaf(ONE ? (g.diag_cols ? dc[r] : dg[fi]) : g.ca, x[r] * (1.f / (1 << kUnitX)), v[r]);
     }
     if (KIND == LAST) {
       if (i >= g.R || j >= g.C) continue;
@@ -529,9 +527,9 @@ dfp_status launch_mm(int32_t id, const MmPlan& p, int32_t batch, MmArgs& g, hipS
   });
 }
 
-// Largest unit of a I + B that keeps it at 32768 or less for |X| <= sqrt(2).
+// Largest unit of B that keeps it at 32768 or less for |X| <= sqrt(2).
 float unit_b(const float* coef) {
-  const double most = std::fabs((double)coef[0]) + std::fabs((double)coef[1]) * 2. + std::fabs((double)coef[2]) * 4.;
+  const double most = std::fabs((double)coef[1]) * 2. + std::fabs((double)coef[2]) * 4.;
   int s = 12;
   while (s > 0 && most * (double)(1 << s) > 32768.) --s;
   return (float)(1 << s);
@@ -580,7 +578,7 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
     g.ldr = g.ldc = p.rp * p.e;
     g.sr = g.sc = ss;
     if ((rc = launch_mm<P, GRAM, 0, false>(K_ORTHO_GRAM, p.mgram, d.batch, g, st)) != DFP_OK) return rc;
-    // B = b A + c A A (and a on its diagonal)
+    // B = b A + c A A
     g.a = g.b = g.old = aa;
     g.lda = g.ldb = p.rp * p.e;
     g.sa = g.sb = ss;
@@ -589,7 +587,7 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
     g.uout = ub;
     g.rowop = g.colop = bb;
     if ((rc = launch_mm<P, POLY, 0, false>(K_ORTHO_POLY, p.mpoly, d.batch, g, st)) != DFP_OK) return rc;
-    // X = (a I + B) X, in the caller's orientation: rows of B by rows of X^T, or rows of X by rows of B
+    // X = a X + B X, in the caller's orientation: rows of B by rows of X^T, or rows of X by rows of B
     uint8_t *from = step[s & 1], *to = step[(s + 1) & 1];
     g.a = p.tall ? from : bb;
     g.b = p.tall ? bb : from;

@@ -102,6 +102,26 @@ def test_zero_and_not_finite_matrices_of_a_batch(t):
         assert_near(got[i], ref.newton_schulz(xf[i], [COEF] * 5, np.float32(1e-7)), TOL[t], t)
 
 
+@pytest.mark.parametrize("r,c", [(256, 256), (300, 700), (700, 300)])
+def test_strong_directions_above_weak_ones(r, c):
+    """FP32 results are as near as FP32 products bring them: at most twice as far from
+    64 bits as the same iteration in FP32 (an operand of two f16 numbers carries 2^-23
+    of a value, FP32 2^-24)."""
+    rng = np.random.default_rng(6)
+    x = 0.1 * rng.standard_normal((r, c)) * np.exp(rng.standard_normal((r, 1)))
+    x = (x + rng.standard_normal((r, 32)) @ rng.standard_normal((32, c)))[None].astype(np.float32)
+    got, xf = run(x, "f32")
+    want = ref.newton_schulz(xf[0], [COEF] * 5, np.float32(1e-7))
+    u = torch.from_numpy(xf[0] if r <= c else np.ascontiguousarray(xf[0].T))
+    u = (u.double() / (u.double().norm() + 1e-7)).float()
+    for _ in range(5):
+        a = u @ u.T
+        u = COEF[0] * u + (COEF[1] * a + COEF[2] * (a @ a)) @ u
+    plain = u.numpy() if r <= c else u.numpy().T
+    off = [np.linalg.norm(y - want) / np.linalg.norm(want) for y in (got[0], plain)]
+    assert off[0] <= 2 * off[1], off
+
+
 @pytest.mark.parametrize("scale", [1e-30, 1e-4, 1e15, 1e33])
 def test_magnitudes(scale):
     """The norm is taken in 64 bits: squares neither overflow nor vanish."""
