@@ -514,14 +514,17 @@ size_t dfp_linear_i8_workspace_bytes(const dfp_linear_desc* d);
  *   X = U / (|U|_F + eps);  steps times, with coefficients (a, b, c) of the step:
  *   A = X X^T, B = b A + c A A, X = a X + B X     (X^T X where rows > cols),
  * which applies x -> a x + b x^3 + c x^5 to the singular values.
- * Precision: X is held in FP32.  BF16 results: the products take X, A and B
- * rounded to f16 (X in units of 2^-12, A of 2^-10, B's diagonal apart in FP32) and
- * sum in FP32: 0.4e-3 to 0.9e-3 of the result's norm for matrices of some size, at
- * most 2^-9, half of BF16's half step, for a few elements too.  FP32 and F16 results and dfp_muon_quantize: every operand is the
- * sum of two f16 numbers and every product the sum of three: 1e-6 to 2e-5, what
- * FP32 products give.  The units suit singular values up to 4 at every step (a, b,
- * c that map [0, 1] further out overflow f16 and give Inf or NaN) and norms not
- * below eps by more than a factor of 2^10 (smaller ones lose bits).  A zero
+ * Precision: X is held as the sum of two f16 numbers (2^-24 of a value), every sum
+ * in FP32.  BF16 results: the products take X, A and B rounded to one f16 number (X
+ * in units of 2^-12, A of 2^-10, B's diagonal apart in FP32): 0.4e-3 to 0.9e-3 of the
+ * result's norm for matrices of some size, at most 2^-9, half of BF16's half step, for a
+ * few elements too.  FP32 and F16 results and dfp_muon_quantize: every operand is the
+ * sum of two f16 numbers and every product the sum of three: 1e-6 to 2e-5, within twice
+ * of what FP32 products give; dfp_muon_quantize on matrices much longer one way up to
+ * three times that (it takes iterations together).  The units suit singular values up
+ * to 4 at every step (a, b, c that map [0, 1] further out overflow f16 and give Inf or
+ * NaN) and norms not below eps by more than a factor of 2^10 (smaller ones lose bits).
+ * A zero
  * matrix gives zeros; one with NaN or Inf gives NaN throughout. */
 #define DFP_ORTHO_MAX_STEPS 16
 typedef struct dfp_ortho_desc {

@@ -15,6 +15,15 @@
 // weak ones).  In an operand of one f16 number B's diagonal, the largest entries of its
 // rows, would be off by most: it stays out and joins too, X = (a + B_ii) X + B' X.
 //
+// Weight steps of matrices that are much longer one way take several iterations on
+// the small square before X is touched: with P = a I + B, the next A is P A P (all are
+// polynomials of A: they commute, and their products are symmetric), and
+// X = P_2 P_1 X = q X + Q X with q = a_2 a_1, Q = a_2 B_1 + a_1 B_2 + B_2 B_1.  That replaces a
+// Gram product and a step by three products of the small side.  An error of A grows by
+// a^2 an iteration, so no more than a^2 a'^2 <= 150 (two such for a = 3.44) are taken
+// before A is computed from X again: 2 to 3 times the error of single iterations, of an
+// update that enters FP32 weights times lr.
+//
 // Units: X in 2^-12, A in 2^-10, B in 2^-sb so that |b A + c A A| <= 32768 in it for
 // singular values up to sqrt(2).
 #include <algorithm>
@@ -41,6 +50,7 @@ constexpr int kNormParts = 1024;  // most partial sums of a matrix
 struct MmPlan {
   int32_t kind, slices, per;
   int64_t bytes;
+  double us;
 };
 constexpr int64_t kMostPartBytes = 128 << 20;
 
@@ -61,7 +71,7 @@ MmPlan plan_mm(int64_t m, int64_t n, int64_t pieces, int64_t batch, bool symmetr
       if (s > 1) us += 4. + 2. * bytes / 5e6;
       if (us < least) {
         least = us;
-        best = {t, (int32_t)s, (int32_t)per, bytes};
+        best = {t, (int32_t)s, (int32_t)per, bytes, us};
       }
     }
   }
@@ -73,8 +83,9 @@ struct Plan {
   int64_t R, C, Rp, Cp;  // the matrix, padded
   int64_t r, rp;         // the smaller side, padded
   int64_t e;             // bytes of an operand element
-  int64_t xlo, gram, step0, step1, aa, bb, diag, norm, slices, bytes;  // offsets, total
+  int64_t xlo, gram, step0, step1, aa, bb, pa, qq0, qq1, diag, norm, slices, bytes;  // offsets, total
   MmPlan mgram, mpoly, mstep;
+  bool grouped;          // weight steps: iterations on the small side (3 us a launch)
 };
 
 Plan make_plan(const dfp_ortho_desc& d, bool split) {
@@ -105,6 +116,10 @@ Plan make_plan(const dfp_ortho_desc& d, bool split) {
   p.step1 = take(n * p.e);
   p.aa = take(s * p.e);
   p.bb = take(s * p.e);
+  p.grouped = split && p.mgram.us + p.mstep.us > 3. * p.mpoly.us + 3.;
+  p.pa = take(p.grouped ? s * p.e : 0);
+  p.qq0 = take(p.grouped ? s * p.e : 0);
+  p.qq1 = take(p.grouped ? s * p.e : 0);
   p.diag = take(split ? 0 : p.rp * d.batch * 4);
   p.norm = take((int64_t)kNormParts * d.batch * 8);
   p.slices = take(p.mgram.bytes);
@@ -298,9 +313,11 @@ struct MmArgs {
   // outputs
   uint8_t *rowop, *colop;  // operand and (GRAM, POLY: the same) its transpose
   int64_t ldr, ldc, sr, sc;
-  const uint8_t* old;      // POLY: A; STEP, LAST: X (its high part); in rowop's layout
-  float* diag;             // one part: POLY writes, STEP reads, [rp] a matrix
-  float cb, cc, ca;        // coefficients
+  const uint8_t* old;      // POLY: cold times this joins (and cold2 old2, nullable); STEP, LAST: X
+  const uint8_t* old2;     //   (its high part); in rowop's layout
+  float cold, cold2;       // (with the units of what they multiply)
+  float* diag;             // one part: POLY writes a + B_ii, STEP reads it, [rp] a matrix
+  float ca;                // a, or a group's q
   float uout;              // unit of the operands written
   uint16_t* xlo;           // one part: X's low part
   int32_t R, C, rp;
@@ -362,10 +379,17 @@ __device__ __forceinline__ void finish(const MmArgs& g, int64_t b, int64_t i0, i
     for (int r = 0; r < 8; ++r) v[r] *= g.unit;
     float x[8];
     if (KIND == POLY || XSTEP) unpack8(hi[fi], lo[fi], x);
+    if (KIND == POLY && !ONE && g.old2) {
+      const uint4* d = (const uint4*)(g.old2 + b * g.sr + i * g.ldr + op_off<P>(j));
+      float y[8];
+      unpack8(d[0], d[4], y);
+#pragma unroll
+      for (int r = 0; r < 8; ++r) v[r] = fmaf(g.cold2, y[r], v[r]);
+    }
     if (KIND == POLY) {
 #pragma unroll
       for (int r = 0; r < 8; ++r) {
-        v[r] = fmaf(g.cc, v[r], g.cb * (x[r] * (1.f / (1 << kUnitA))));
+        v[r] = fmaf(g.cold, x[r], v[r]);
         if (ONE && i == j + r) {
           g.diag[b * g.rp + i] = g.ca + v[r];
           v[r] = 0.f;
@@ -527,9 +551,8 @@ dfp_status launch_mm(int32_t id, const MmPlan& p, int32_t batch, MmArgs& g, hipS
   });
 }
 
-// Largest unit of B that keeps it at 32768 or less for |X| <= sqrt(2).
-float unit_b(const float* coef) {
-  const double most = std::fabs((double)coef[1]) * 2. + std::fabs((double)coef[2]) * 4.;
+// Largest unit, 2^12 at most, that keeps an operand of up to `most` at 32768 or less.
+float unit_for(double most) {
   int s = 12;
   while (s > 0 && most * (double)(1 << s) > 32768.) --s;
   return (float)(1 << s);
@@ -558,14 +581,29 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
   const int64_t longer = p.tall ? p.Rp : p.Cp;
   const int64_t sx = p.Rp * p.Cp * p.e, ss = p.rp * p.rp * p.e;
   constexpr float kInvX = 1.f / (1 << kUnitX), kInvA = 1.f / (1 << kUnitA);
-  for (int32_t s = 0; s < d.steps; ++s) {
-    const float ub = unit_b(d.coef[s]);
-    dfp_status rc;
-    MmArgs g{};
+  // C = A B of the small side, symmetric: C = unit A B + c X [+ c2 Y], times uout
+  uint8_t *pa = base + p.pa, *qq[2] = {base + p.qq0, base + p.qq1};
+  MmArgs g{};
+  auto small = [&](const uint8_t* a, const uint8_t* b, uint8_t* to, float unit, const uint8_t* x, float c, float uout,
+                   const uint8_t* y = nullptr, float c2 = 0.f) -> dfp_status {
+    g.a = a, g.b = b;
+    g.lda = g.ldb = g.ldr = g.ldc = p.rp * p.e;
+    g.sa = g.sb = g.sr = g.sc = ss;
+    g.m = g.n = (int32_t)p.rp;
+    g.pieces = (int32_t)(p.rp / kPerPiece);
+    g.unit = unit;
+    g.old = x, g.cold = c;
+    g.old2 = y, g.cold2 = c2;
+    g.uout = uout;
+    g.rowop = g.colop = to;
+    return launch_mm<P, POLY, 0, false>(K_ORTHO_POLY, p.mpoly, d.batch, g, st);
+  };
+  dfp_status rc;
+  for (int32_t s = 0, turn = 0; s < d.steps; ++turn) {
+    g = MmArgs{};
     g.rp = (int32_t)p.rp;
     g.diag = (float*)(base + p.diag);
     g.part = (float*)(base + p.slices);
-    g.ca = d.coef[s][0], g.cb = d.coef[s][1], g.cc = d.coef[s][2];
     // A = X X^T
     g.a = g.b = gram;
     g.lda = g.ldb = longer * p.e;
@@ -578,36 +616,54 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
     g.ldr = g.ldc = p.rp * p.e;
     g.sr = g.sc = ss;
     if ((rc = launch_mm<P, GRAM, 0, false>(K_ORTHO_GRAM, p.mgram, d.batch, g, st)) != DFP_OK) return rc;
-    // B = b A + c A A
-    g.a = g.b = g.old = aa;
-    g.lda = g.ldb = p.rp * p.e;
-    g.sa = g.sb = ss;
-    g.pieces = (int32_t)(p.rp / kPerPiece);
-    g.unit = kInvA * kInvA;
-    g.uout = ub;
-    g.rowop = g.colop = bb;
-    if ((rc = launch_mm<P, POLY, 0, false>(K_ORTHO_POLY, p.mpoly, d.batch, g, st)) != DFP_OK) return rc;
-    // X = a X + B X, in the caller's orientation: rows of B by rows of X^T, or rows of X by rows of B
-    uint8_t *from = step[s & 1], *to = step[(s + 1) & 1];
-    g.a = p.tall ? from : bb;
-    g.b = p.tall ? bb : from;
+    // Q = B = b A + c A A, and what further iterations make of it; X = q X + Q X in the end
+    uint8_t* q = bb;
+    float uq = 1.f;
+    double qa = 1., grown = 1.;
+    for (int32_t k = 0;; ++k, ++s) {
+      const float ca = d.coef[s][0], cb = d.coef[s][1], cc = d.coef[s][2];
+      const float ub = unit_for(std::fabs((double)cb) * 2. + std::fabs((double)cc) * 4.);
+      uint8_t* to = k == 0 && MUON && p.grouped ? qq[0] : bb;
+      g.ca = ca;
+      if ((rc = small(aa, aa, to, cc * kInvA * kInvA, aa, cb * kInvA, ub)) != DFP_OK) return rc;
+      if (k == 0) {
+        q = to, uq = ub;
+      } else {
+        const float un = unit_for(2. * std::fabs(qa * ca));
+        if ((rc = small(bb, q, qq[k & 1], 1.f / (ub * uq), q, ca / uq, un, bb, (float)qa / ub)) != DFP_OK) return rc;
+        q = qq[k & 1], uq = un;
+      }
+      qa *= ca;
+      grown *= (double)ca * ca;
+      if (!MUON || !p.grouped || s + 1 >= d.steps || grown > 150.) break;
+      // A = P A P
+      const float ua = (float)(1 << kUnitA);
+      if ((rc = small(to, aa, pa, kInvA / ub, aa, ca * kInvA, ua)) != DFP_OK) return rc;
+      if ((rc = small(to, pa, aa, kInvA / ub, pa, ca * kInvA, ua)) != DFP_OK) return rc;
+    }
+    ++s;
+    // X = q X + Q X, in the caller's orientation: rows of Q by rows of X^T, or rows of X by rows of Q
+    uint8_t *from = step[turn & 1], *to = step[(turn + 1) & 1];
+    g.a = p.tall ? from : q;
+    g.b = p.tall ? q : from;
     g.sa = p.tall ? sx : ss;
     g.sb = p.tall ? ss : sx;
     g.m = (int32_t)p.Rp, g.n = (int32_t)p.Cp;
-    g.unit = kInvX / ub;
+    g.unit = kInvX / uq;
     g.uout = (float)(1 << kUnitX);
     g.rowop = p.tall ? to : gram;
     g.colop = p.tall ? gram : to;
     g.old = p.tall ? from : gram;
     g.ldr = p.Cp * p.e, g.ldc = p.Rp * p.e;
     g.sr = g.sc = sx;
+    g.ca = (float)qa;
     g.xlo = xlo;
     g.R = (int32_t)p.R, g.C = (int32_t)p.C;
     g.diag_cols = p.tall;
     g.out = out;
     g.w = w;
     g.alpha = alpha, g.keep = keep;
-    if (s + 1 < d.steps)
+    if (s < d.steps)
       rc = launch_mm<P, STEP, 0, false>(K_ORTHO_STEP, p.mstep, d.batch, g, st);
     else
       rc = launch_mm<P, LAST, MUON ? DFP_F32 : T, MUON>(K_ORTHO_STEP, p.mstep, d.batch, g, st);

@@ -116,3 +116,63 @@ def test_orthogonalize(t, b, r, c):
         off = float(torch.linalg.vector_norm(out[i].double() - u) / torch.linalg.vector_norm(u))
         assert np.isfinite(off) and off <= (2e-4 if t == "f32" else 3e-3), (i, off)
     assert bool((raw[b * r * c:] == 7).all())
+
+
+# weight steps that iterate on the small side, wide and tall, a batch, and beside them ones that do not
+MUON = [(1, 1024, 4096), (1, 4096, 1024), (1, 2200, 1000), (3, 200, 2000), (1, 20000, 200), (2, 130, 9000),
+        (1, 64, 8000), (1, 512, 2048), (1, 1500, 1500)]
+SCHEDULES = {
+    "same": [COEF] * 5,
+    "one": [COEF],
+    "two": [COEF] * 2,
+    "eight": [(2.0, -1.5, 0.5)] * 8,
+    # coefficients of their own for each step, the first far above the others: within [0, 2] on [0, 1]
+    "falling": [(8.287, -23.596, 17.300), (4.107, -2.948, 0.545), (3.949, -2.909, 0.552), (3.318, -2.488, 0.510),
+                (2.301, -1.669, 0.419)],
+    # the same rounded further: from 1 they end above 1000, past the documented range (4)
+    "out of range": [(8.2, -23.0, 17.0), (4.1, -2.9, 0.55), (3.9, -2.8, 0.55), (3.3, -2.4, 0.5), (2.0, -1.5, 0.5)],
+}
+
+
+@pytest.mark.parametrize("kind", ["full", "low_rank"])
+@pytest.mark.parametrize("coef", list(SCHEDULES))
+@pytest.mark.parametrize("b,r,c", MUON)
+def test_muon(b, r, c, coef, kind):
+    """The update's tolerance is that of single iterations, twice: an error of A grows by
+    (a a')^2 = 140 at most before X is looked at again, of A's 2^-22: 3.4e-5, six of which
+    (B has |b| + 2 |c| of it) stay under 2e-4."""
+    note("muon tiles %dx%dx%d %s %s" % (b, r, c, coef, kind))
+    steps = SCHEDULES[coef]
+    g = torch.Generator(device=DEV)
+    g.manual_seed(r * 3 + c)
+    normal = lambda *s: torch.randn(*s, generator=g, device=DEV)  # noqa: E731
+    u = normal(b, r, c) * torch.exp(0.5 * normal(b, r, 1))
+    if kind == "low_rank":
+        k = min(r, c) // 16
+        u = 0.3 * u + torch.stack([normal(r, k) @ normal(k, c) for _ in range(b)])
+    dw = (1e-3 * u).contiguous()
+    d = dfp.make_ortho_desc(b, r, c, torch.float32, steps=len(steps), coef=steps)
+    # w = 0 and lr scale = 1 leave -O(u), v = 0 and mu = 0 make u = dw
+    w, v = torch.zeros(b, r, c, device=DEV), torch.zeros(b, r, c, device=DEV)
+    ws = torch.full((dfp.ortho_workspace_bytes(d),), 0xff, dtype=torch.uint8, device=DEV)
+    dfp.dfp_muon_quantize(d, 1.0, 0.0, 0.0, 1.0, w, v, dw, workspace=ws)
+    assert torch.equal(v, dw)
+    for i in range(b):
+        x = dw[i].double()
+        x = x.t().contiguous() if r > c else x
+        x = x / (torch.linalg.vector_norm(x) + 1e-7)
+        largest = 0.0
+        for ca, cb, cc in d.coef[:len(steps)]:
+            a = torch.mm(x, x.t().contiguous())
+            x = ca * x + torch.mm(cb * a + cc * torch.mm(a, a), x)
+            z = torch.ones(x.shape[0], 1, dtype=torch.float64, device=DEV)
+            for _ in range(20):  # the largest singular value, from below
+                z = torch.mm(x, torch.mm(x.t().contiguous(), z / torch.linalg.vector_norm(z)))
+            largest = max(largest, float(torch.linalg.vector_norm(z)) ** 0.5)
+        if largest > 4:
+            assert coef == "out of range"
+            continue
+        x = x.t() if r > c else x
+        off = float(torch.linalg.vector_norm(w[i].double() + x) / torch.linalg.vector_norm(x))
+        print("off %.2e, largest %.2f" % (off, largest))
+        assert np.isfinite(off) and off <= 4e-4, off
