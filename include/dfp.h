@@ -461,7 +461,9 @@ dfp_status dfp_sgd_quantize(int64_t n, float lr, float mu, float wd, int32_t bit
  * padding bytes ZERO (dfp_quantize_i8 writes them).  Transposed operands (wqt,
  * xqt) are the same integers as [cols][dfp_i8_ld(rows)].  Tensors and INT8
  * operands 16-byte aligned, scales and biases 4-byte.
- * Sizes: every dimension >= 1; k (and n for backward-data, m for
+ * Outputs overlap neither inputs nor each other.
+ * Sizes: every dimension >= 1 and at most 2^26, the product of any two, each
+ * rounded up to 128, at most 2^36; k (and n for backward-data, m for
  * backward-weights: the summed one) at most DFP_I8_MAX_SUM, so that no INT32
  * sum overflows whatever the integers are. */
 typedef enum dfp_type { DFP_F32 = 0, DFP_BF16 = 1, DFP_F16 = 2 } dfp_type;
@@ -480,7 +482,8 @@ int64_t dfp_i8_ld(int64_t cols);
 
 /* Rows of src [rows][cols] (a dfp_type) to INT8.  q: [rows][dfp_i8_ld(cols)];
  * scale: FP32 [rows]; qt (nullable): the transpose, [cols][dfp_i8_ld(rows)].
- * rows and cols at most 2^31 - 256 each, rows * ld at most 2^40. */
+ * rows and cols at most 2^31 - 256, their product, each rounded up to 128, at most
+ * 2^36. */
 dfp_status dfp_quantize_i8(int64_t rows, int64_t cols, int32_t type, int32_t rounding, uint64_t seed, int32_t role,
                            const void* src, int8_t* q, float* scale, int8_t* qt, void* stream);
 
@@ -524,12 +527,11 @@ size_t dfp_linear_i8_workspace_bytes(const dfp_linear_desc* d);
  * three times that (it takes iterations together).  The units suit singular values up
  * to 4 at every step (a, b, c that map [0, 1] further out overflow f16 and give Inf or
  * NaN) and norms not below eps by more than a factor of 2^10 (smaller ones lose bits).
- * A zero
- * matrix gives zeros; one with NaN or Inf gives NaN throughout. */
+ * A zero matrix gives zeros; one with NaN or Inf gives NaN throughout. */
 #define DFP_ORTHO_MAX_STEPS 16
 typedef struct dfp_ortho_desc {
-  int32_t batch, rows, cols; /* >= 1; rows, cols <= 65536; batch <= 65535; batch
-                                times the padded matrix at most 2^40 elements  */
+  int32_t batch, rows, cols; /* >= 1; rows, cols <= 65536; batch <= 65535; batch *
+                                rows * cols, both rounded up to 128, <= 2^36   */
   int32_t type;              /* dfp_type of x and out, or of dw                */
   int32_t steps;             /* 1 .. DFP_ORTHO_MAX_STEPS                       */
   float eps;                 /* finite, > 0                                    */
@@ -548,7 +550,8 @@ dfp_status dfp_orthogonalize(const dfp_ortho_desc* d, const void* x, void* out, 
  * with lr scale and 1 - lr wd rounded to FP32 on the host, O as above; then, with
  * wq, the rows of the new w (batch * rows of them) to INT8 as dfp_quantize_i8
  * does (NEAREST): wq [batch*rows][ld(cols)], sw FP32 [batch*rows], wqt (nullable,
- * batch = 1 only) [cols][ld(rows)].  wq and sw both or neither. */
+ * batch = 1 only) [cols][ld(rows)].  wq and sw both or neither.  None of them may
+ * overlap another. */
 dfp_status dfp_muon_quantize(const dfp_ortho_desc* d, float lr, float mu, float wd, float scale, int32_t nesterov,
                              float* w, float* v, const void* dw, int8_t* wq, float* sw, int8_t* wqt, void* workspace,
                              size_t ws_bytes, void* stream);

@@ -11,8 +11,10 @@
 namespace dfp {
 namespace {
 
-constexpr int64_t kMaxElems = (int64_t)1 << 37;  // of a tensor or operand: more than the card holds
-constexpr int64_t kMaxSide = ((int64_t)1 << 31) - 256;
+// Elements of a tensor or operand, and sides of a product: beyond what the card holds,
+// and few enough that no launch reaches 2^32 threads (a third of it at worst).
+constexpr int64_t kMaxElems = (int64_t)1 << 36;
+constexpr int64_t kMaxSide = ((int64_t)1 << 31) - 256, kMaxProductSide = 1 << 26;
 
 bool aligned(const void* p, uintptr_t a) { return ((uintptr_t)p % a) == 0; }
 bool type_ok(int32_t t) { return t >= DFP_F32 && t <= DFP_F16; }
@@ -21,9 +23,8 @@ bool i8_rounding_ok(int32_t r) { return r == DFP_ROUND_NEAREST || r == DFP_ROUND
 dfp_status linear_checks(const dfp_linear_desc* d) {
   if (!d) return DFP_ERR_NULL;
   if (!type_ok(d->type) || !i8_rounding_ok(d->rounding)) return DFP_ERR_PARAM;
-  if (d->m < 1 || d->n < 1 || d->k < 1 || d->m > kMaxSide || d->n > kMaxSide || d->k > kMaxSide) return DFP_ERR_SHAPE;
+  if (d->m < 1 || d->n < 1 || d->k < 1 || std::max({d->m, d->n, d->k}) > kMaxProductSide) return DFP_ERR_SHAPE;
   const int64_t m = i8_ld(d->m), n = i8_ld(d->n), k = i8_ld(d->k);
-  // (each factor below 2^31: no overflow)
   if (m * n > kMaxElems || m * k > kMaxElems || n * k > kMaxElems) return DFP_ERR_SHAPE;
   return DFP_OK;
 }

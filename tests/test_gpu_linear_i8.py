@@ -236,6 +236,25 @@ def test_layer_stochastic(m, n, k):
     layer.check()
 
 
+@pytest.mark.parametrize("rounding", ["nearest", "stochastic"])
+@pytest.mark.parametrize("t", list(TYPES))
+@pytest.mark.parametrize("m,k", [(1, 1), (1, 300), (2, 77), (2, 300), (1, 4097), (2, 8200), (1, 20001), (1, 40000),
+                                 (2, 20001), (3, 300)])
+def test_few_tokens(m, k, t, rounding):
+    """One or two tokens run in one launch, which quantises them as the other calls do."""
+    layer = Layer(m, 50, k, t, rounding=rounding, seed=7, zero_rows=False)
+    if m == 2:
+        layer.tx[1] = 0
+        layer.x[1] = 0
+    layer.run()
+    y = torch.empty_like(layer.y)
+    dfp.dfp_linear_i8_fwd(layer.d, layer.tx, layer.twq, layer.tsw, y, bias=layer.tb, workspace=layer.ws)
+    assert torch.equal(y.float(), layer.y.float())
+    layer.tx[0, k // 2] = float("nan")
+    dfp.dfp_linear_i8_fwd(layer.d, layer.tx, layer.twq, layer.tsw, y, bias=layer.tb, workspace=layer.ws)
+    assert torch.isnan(y[0]).all() and torch.equal(y[1:].float(), layer.y[1:].float())
+
+
 @pytest.mark.parametrize("m", [1, 6, 40, 300])
 def test_forward_without_saved_tensors(m):
     layer = Layer(m, 70, 300, "bf16")

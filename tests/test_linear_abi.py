@@ -44,7 +44,7 @@ def test_quantize_refusals(dl):
     assert quantize(dl, rounding=2) == quantize(dl, rounding=3) == quantize(dl, rounding=-1) == dl.ERR_PARAM
     assert quantize(dl, role=5) == quantize(dl, role=-1) == dl.ERR_PARAM
     assert quantize(dl, rows=0) == quantize(dl, cols=0) == quantize(dl, cols=2 ** 31) == dl.ERR_SHAPE
-    assert quantize(dl, rows=1 << 20, cols=1 << 20) == dl.ERR_SHAPE
+    assert quantize(dl, rows=1 << 20, cols=1 << 20) == quantize(dl, rows=(1 << 18) + 1, cols=1 << 18) == dl.ERR_SHAPE
     assert quantize(dl, src=FAKE + 8) == quantize(dl, q=FAKE + 8) == quantize(dl, qt=FAKE + 4) == dl.ERR_ALIGN
     assert quantize(dl, s=FAKE + 2) == dl.ERR_ALIGN
 
@@ -86,7 +86,7 @@ def test_linear_refusals(dl, name):
     for field, value in (("type", 3), ("type", -1), ("rounding", 2), ("rounding", 3)):
         assert call(dl, name, desc(dl, **{field: value})) == dl.ERR_PARAM, field
     for field in "mnk":
-        for value in (0, -1, 2 ** 31 - 255):
+        for value in (0, -1, 2 ** 26 + 1, 2 ** 31 - 1):
             assert call(dl, name, desc(dl, **{field: value})) == dl.ERR_SHAPE, field
     assert call(dl, name, desc(dl, **{SUMMED[name]: 131072})) == dl.ERR_SHAPE
     assert call(dl, name, desc(dl, m=1 << 20, n=1 << 20)) == dl.ERR_SHAPE
@@ -128,7 +128,7 @@ def test_ortho_refusals(dl):
             d.steps = 4  # a step that is not taken is not looked at
             assert f(dl, d, wsn=0) == dl.ERR_WORKSPACE
         for change in (dict(batch=0), dict(rows=0), dict(cols=-1), dict(rows=65537), dict(cols=65537),
-                       dict(batch=65536), dict(batch=33, rows=65536, cols=65536)):
+                       dict(batch=65536), dict(batch=17, rows=65536, cols=65536)):
             d = dl.make_ortho_desc(2, 30, 40)
             for k, v in change.items():
                 setattr(d, k, v)
