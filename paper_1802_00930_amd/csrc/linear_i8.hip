@@ -295,7 +295,7 @@ I8Plan plan_gemm_i8(int64_t m, int64_t n, int64_t k) {
       const int64_t per = (pieces + slices - 1) / slices, used = (pieces + per - 1) / per;
       const int64_t bytes = used > 1 ? used * m * n * 4 : 0;
       if (bytes > kMostPartBytes) break;
-      double us = 2.5 + tile_us(kind, false, tiles * used, per) * (m <= kFewRows ? 1.25 : 1.);
+      double us = tile_us(kind, false, tiles * used, per, m <= kFewRows ? 1.25 : 1.);
       if (used > 1) us += 4. + 2. * bytes / 4e6;
       if (us < least) {
         least = us;

@@ -217,11 +217,12 @@ struct MmaTile {
   }
 };
 
-// The tiles in use, and a CU's time for a piece of one: `alone` if it has one tile,
-// `busy` a tile if it has several (us; I8 and F16, F16X2; 512 x 512 x 8192 bytes and
-// 8192^2 x 8192).  Outputs of a tile per time fall with its side, but a product takes
-// as long as the CU with the most tiles, and 256 CUs are filled in steps: 3008 x 3008
-// x 4096 takes 63.6, 42.7, 46.8, 55.0, 59.1 and 65.3 with these.
+// The tiles in use and an estimate of a product's time (us), from products of 64 to 1024
+// tiles (`tiles` / 256 rounded up: the most a CU has) at reductions of 32 and 96 pieces:
+//   start + (rounds - 1) start_round + pieces (piece, from 128 to 256 tiles rising to
+//   piece_full, + (rounds - 1) piece_round)
+// for I8 and F16, and for F16X2.  Outputs of a tile per time rise with its side, but so
+// does what starts and ends it, and 256 CUs are filled in steps.
 template <int TM_, int TN_, int WM_, int WN_, int S_, int KG_ = 1>
 struct TileShape {
   static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, S = S_, KG = KG_;
@@ -229,17 +230,25 @@ struct TileShape {
   template <Prod P>
   using Tile = MmaTile<P, TM, TN, WM, WN, S, KG>;
 };
+struct TileCost {
+  double start, start_round, piece, piece_full, piece_round;
+};
 struct TileKind {
   int32_t tm, tn;
-  double alone[2], busy[2], once;  // once: whatever the reduction (the groups' sums)
+  TileCost cost[2];
 };
 constexpr TileKind kTileKinds[] = {
-    {256, 256, {1.38, 1.74}, {1.78, 2.22}, 0.}, {192, 192, {0.85, 1.05}, {1.14, 1.42}, 0.},
-    {192, 128, {0.67, 0.75}, {0.67, 0.88}, 0.}, {128, 128, {0.58, 0.64}, {0.58, 0.62}, 0.},
-    {96, 96, {0.39, 0.44}, {0.39, 0.46}, 0.},   {64, 64, {0.31, 0.33}, {0.18, 0.20}, 0.},
-    {64, 64, {0.24, 0.26}, {0.24, 0.26}, 0.5},  // two groups
+    {256, 256, {{14.0, 12.5, 1.23, 1.61, 1.60}, {14.5, 13.0, 1.55, 2.14, 2.12}}},
+    {192, 192, {{8.6, 7.0, 0.77, 0.96, 0.95}, {8.5, 7.5, 0.96, 1.29, 1.25}}},
+    {192, 128, {{5.5, 5.5, 0.71, 0.76, 0.58}, {6.8, 5.0, 0.70, 0.92, 0.80}}},
+    {128, 128, {{5.0, 4.0, 0.63, 0.63, 0.41}, {6.0, 4.0, 0.61, 0.67, 0.56}}},
+    {96, 96, {{4.0, 2.3, 0.35, 0.37, 0.36}, {4.5, 2.3, 0.39, 0.43, 0.44}}},
+    {64, 64, {{1.0, 1.8, 0.28, 0.30, 0.16}, {1.7, 1.4, 0.29, 0.30, 0.17}}},
+    {64, 64, {{2.3, 2.2, 0.20, 0.21, 0.20}, {3.1, 2.5, 0.20, 0.22, 0.21}}},     // two groups each
+    {128, 128, {{6.5, 5.0, 0.47, 0.53, 0.51}, {7.5, 6.5, 0.49, 0.59, 0.60}}},
+    {96, 96, {{5.5, 4.0, 0.30, 0.29, 0.31}, {6.5, 4.3, 0.30, 0.33, 0.36}}},
 };
-constexpr int kTileKindCount = 7;
+constexpr int kTileKindCount = 9;
 template <class F>
 dfp_status with_tile(int32_t kind, F f) {
   switch (kind) {
@@ -249,12 +258,18 @@ dfp_status with_tile(int32_t kind, F f) {
     case 3: return f(TileShape<128, 128, 2, 2, 2>());
     case 4: return f(TileShape<96, 96, 2, 3, 3>());
     case 5: return f(TileShape<64, 64, 2, 2, 3>());
-    default: return f(TileShape<64, 64, 2, 2, 3, 2>());
+    case 6: return f(TileShape<64, 64, 2, 2, 3, 2>());
+    case 7: return f(TileShape<128, 128, 2, 2, 2, 2>());
+    default: return f(TileShape<96, 96, 2, 3, 3, 2>());
   }
 }
-inline double tile_us(const TileKind& k, bool split, int64_t tiles, int64_t pieces) {
-  const double many = (double)((tiles + 255) / 256) * k.busy[split];
-  return (double)pieces * (many > k.alone[split] ? many : k.alone[split]) + k.once;
+// slow: what the reduction takes more when operands come from memory.
+inline double tile_us(const TileKind& k, bool split, int64_t tiles, int64_t pieces, double slow = 1.) {
+  const TileCost& c = k.cost[split];
+  const double more = (double)((tiles + 255) / 256 - 1);
+  const double full = tiles >= 256 ? 1. : tiles <= 128 ? 0. : (double)(tiles - 128) / 128.;
+  return c.start + more * c.start_round +
+         (double)pieces * slow * (c.piece + full * (c.piece_full - c.piece) + more * c.piece_round);
 }
 
 // Consecutive workgroups go round the 8 XCDs, each with an L2 of its own: this turns

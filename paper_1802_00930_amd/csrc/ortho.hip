@@ -45,8 +45,9 @@ constexpr int kBlock = 256;
 constexpr int kUnitX = 12, kUnitA = 10;
 constexpr int kNormParts = 1024;  // most partial sums of a matrix
 
-// A product's tiles and slices by an estimate of its time: tile_us, and slices mean
-// that their sums are written and read (5 TB/s) and a second kernel (4 us).
+// A product's tiles and slices by an estimate of its time: tile_us and 2 us a round for
+// 128 x 128 outputs (which are stored twice, after another pass through LDS); slices
+// mean that their sums are written and read (5 TB/s) and a second kernel (4 us).
 struct MmPlan {
   int32_t kind, slices, per;
   int64_t bytes;
@@ -54,12 +55,18 @@ struct MmPlan {
 };
 constexpr int64_t kMostPartBytes = 128 << 20;
 
+// Tiles of the symmetric products: square, and of two parts not 96 x 96 by one group,
+// which two groups always beat (kTileKinds[4] and [8]).
+constexpr bool has_triangle(int kind, bool split) {
+  return kTileKinds[kind].tm == kTileKinds[kind].tn && !(split && kind == 4);
+}
+
 MmPlan plan_mm(int64_t m, int64_t n, int64_t pieces, int64_t batch, bool symmetric, bool sliceable, bool split) {
   MmPlan best{};
   double least = 1e30;
   for (int t = 0; t < kTileKindCount; ++t) {
     const TileKind& kind = kTileKinds[t];
-    if (symmetric && kind.tm != kind.tn) continue;
+    if (symmetric && !has_triangle(t, split)) continue;
     const int64_t tm = (m + kind.tm - 1) / kind.tm, tn = (n + kind.tn - 1) / kind.tn;
     const int64_t tiles = (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batch;
     for (int64_t s = 1; s <= (sliceable ? 32 : 1) && s <= pieces; ++s) {
@@ -67,7 +74,8 @@ MmPlan plan_mm(int64_t m, int64_t n, int64_t pieces, int64_t batch, bool symmetr
       if (used != s) continue;
       const int64_t bytes = s > 1 ? s * tiles * kind.tm * kind.tn * 4 : 0;
       if (bytes > kMostPartBytes) break;
-      double us = tile_us(kind, split, tiles * s, per);
+      double us = tile_us(kind, split, tiles * s, per) +
+                  2. * ((tiles * s + 255) / 256) * kind.tm * kind.tn / 16384.;
       if (s > 1) us += 4. + 2. * bytes / 5e6;
       if (us < least) {
         least = us;
@@ -534,7 +542,7 @@ dfp_status launch_mm(int32_t id, const MmPlan& p, int32_t batch, MmArgs& g, hipS
   const uint32_t wgs = g.tiles * (uint32_t)batch;
   return with_tile(p.kind, [&](auto shape) -> dfp_status {
     typedef decltype(shape) Q;
-    if constexpr (SYM && Q::TM != Q::TN) {
+    if constexpr (SYM && (Q::TM != Q::TN || (P == Prod::F16X2 && Q::TM == 96 && Q::KG == 1))) {
       return DFP_ERR_PARAM;  // (no plan has it)
     } else {
       if constexpr (KIND == GRAM) {

@@ -11,29 +11,41 @@ from paper_1802_00930_amd import dfp
 
 pytestmark = pytest.mark.gpu
 
-# tile, slices: m, n, k
+# m, n, k: the tile that the estimate chooses, and slices of the reduction
 PRODUCTS = [
-    (66, 16892, 100),      # 96 x 96
-    (1500, 1500, 500),
-    (134, 32975, 200),     # 192 x 192
-    (3000, 3000, 257),
-    (49252, 135, 40),      # 256 x 256
-    (4000, 4090, 300),
-    (33709, 70, 129),      # 192 x 128
-    (3000, 2000, 1000),
-    (68, 26785, 300),      # 128 x 128
-    (2000, 2000, 200),
-    (1100, 1500, 700),     # 64 x 64
-    (65, 3, 1965),         # the same, 16 slices
-    (200, 300, 30000),
-    (69, 2051, 3667),      # 96 x 96, 8
-    (73, 6667, 6926),      # 128 x 128, 4
-    (3258, 67, 15308),     # 192 x 128, 15
-    (3248, 148, 22892),    # 192 x 192, 15
-    (3597, 148, 75337),    # 256 x 256, 16
-    (64, 1, 1),            # rows of a batch
-    (40, 9000, 3000),
-    (24, 5000, 8192),
+    (66, 16892, 100),       # 96 x 96
+    (1500, 1500, 500),      # 96 x 96
+    (134, 32975, 200),      # 192 x 192
+    (3000, 3000, 257),      # 192 x 192
+    (49252, 135, 40),       # 96 x 96
+    (4000, 4090, 300),      # 256 x 256
+    (33709, 70, 129),       # 192 x 128
+    (3000, 2000, 1000),     # 192 x 128
+    (68, 26785, 300),       # 128 x 128
+    (2000, 2000, 200),      # 128 x 128
+    (1100, 1500, 700),      # 64 x 64
+    (65, 3, 1965),          # 64 x 64, 16 slices
+    (200, 300, 30000),      # 64 x 64 by two groups, 8 slices
+    (69, 2051, 3667),       # 64 x 64 by two groups
+    (73, 6667, 6926),       # 64 x 64 by two groups
+    (3258, 67, 15308),      # 64 x 64 by two groups, 2 slices
+    (3248, 148, 22892),     # 128 x 128 by two groups, 4 slices
+    (3597, 148, 75337),     # 192 x 192, 8 slices
+    (64, 1, 1),             # 64 x 64
+    (40, 9000, 3000),       # 64 x 64 by two groups
+    (24, 5000, 8192),       # 64 x 64 by two groups, 2 slices
+    (16720, 17, 3113),      # 96 x 96 by two groups
+    (1091, 20, 63062),      # 64 x 64 by two groups, 8 slices
+    (71, 2105, 8158),       # 96 x 96, 8 slices
+    (195, 2123, 62434),     # 256 x 256, 16 slices
+    (1085, 195, 26458),     # 192 x 128, 16 slices
+    (1077, 102, 50733),     # 128 x 128 by two groups, 16 slices
+    (16503, 97, 1641),      # 128 x 128 by two groups
+    (3151, 130, 26571),     # 192 x 192, 8 slices
+    (99, 4387, 91434),      # 128 x 128, 16 slices
+    (1914, 33, 2132),       # 64 x 64 by two groups
+    (64, 35919, 18),        # rows of a batch
+    (63124, 130, 40),       # 256 x 256
 ]
 
 
@@ -62,32 +74,66 @@ def test_product(m, n, k, t):
     assert bool((raw[m * n:] == 77).all())
 
 
-# Gram, polynomial and step tiles; one f16 number (BF16) or two
+# the tiles of the Gram product, the polynomial and the step, (2) by two groups of waves;
+# operands of one f16 number (BF16) or two
 ORTHO = [
-    ("bf16", 9, 1175, 924),    # 96 x 96
-    ("bf16", 1, 2641, 1146),   # Gram 96 x 96 in slices
-    ("bf16", 9, 875, 977),     # 128 x 128
-    ("bf16", 1, 7154, 1009),   # Gram 128 x 128 in slices
-    ("bf16", 9, 1154, 1109),   # 192 x 192
-    ("bf16", 1, 1312, 14953),  # Gram 192 x 192 in slices
-    ("bf16", 9, 1550, 1928),   # 256 x 256
-    ("bf16", 4, 996, 10316),   # Gram 256 x 256 in slices
-    ("bf16", 9, 134, 1234),    # step 96 x 96
-    ("bf16", 9, 3896, 67),     # step 192 x 128
-    ("bf16", 4, 131, 8562),    # step 192 x 192
-    ("bf16", 9, 6071, 144),    # step 256 x 256
-    ("f32", 9, 1038, 917),     # 96 x 96
-    ("f32", 4, 531, 1469),     # Gram 96 x 96 in slices
-    ("f32", 9, 819, 921),      # 128 x 128
-    ("f32", 1, 849, 4228),     # Gram 128 x 128 in slices
-    ("f32", 9, 1807, 1303),    # 192 x 192
-    ("f32", 1, 9751, 1286),    # Gram 192 x 192 in slices
-    ("f32", 9, 1693, 1632),    # 256 x 256
-    ("f32", 1, 1995, 7899),    # Gram 256 x 256 in slices
-    ("f32", 1, 11162, 130),    # step 96 x 96
-    ("f32", 9, 69, 3646),      # step 192 x 128
-    ("f32", 4, 10127, 129),    # step 192 x 192
-    ("f32", 4, 140, 15184),    # step 256 x 256
+    ("bf16", 9, 1175, 924),    # 96 x 96; 96 x 96; 192 x 128
+    ("bf16", 1, 2641, 1146),   # 64 x 64 (2); 64 x 64 (2); 64 x 64
+    ("bf16", 9, 875, 977),     # 128 x 128 (2); 128 x 128; 128 x 128
+    ("bf16", 1, 7154, 1009),   # 96 x 96 (2), 3 slices; 64 x 64; 192 x 192
+    ("bf16", 9, 1154, 1109),   # 192 x 192; 192 x 192; 256 x 256
+    ("bf16", 1, 1312, 14953),  # 96 x 96 (2), 2 slices; 64 x 64 (2); 192 x 128
+    ("bf16", 9, 1550, 1928),   # 256 x 256; 256 x 256; 256 x 256
+    ("bf16", 4, 996, 10316),   # 192 x 192, 3 slices; 64 x 64; 256 x 256
+    ("bf16", 9, 134, 1234),    # 64 x 64 (2); 64 x 64; 96 x 96
+    ("bf16", 9, 3896, 67),     # 64 x 64, 9 slices; 64 x 64; 192 x 128
+    ("bf16", 4, 131, 8562),    # 64 x 64, 10 slices; 64 x 64; 96 x 96
+    ("bf16", 9, 6071, 144),    # 64 x 64 (2), 4 slices; 64 x 64; 96 x 96
+    ("f32", 9, 1038, 917),     # 96 x 96 (2); 96 x 96 (2); 64 x 64
+    ("f32", 4, 531, 1469),     # 64 x 64 (2); 64 x 64 (2); 128 x 128 (2)
+    ("f32", 9, 819, 921),      # 128 x 128 (2); 128 x 128 (2); 192 x 192
+    ("f32", 1, 849, 4228),     # 64 x 64 (2), 2 slices; 64 x 64 (2); 128 x 128 (2)
+    ("f32", 9, 1807, 1303),    # 192 x 192; 192 x 192; 192 x 128
+    ("f32", 1, 9751, 1286),    # 96 x 96 (2), 2 slices; 64 x 64 (2); 256 x 256
+    ("f32", 9, 1693, 1632),    # 256 x 256; 256 x 256; 192 x 192
+    ("f32", 1, 1995, 7899),    # 96 x 96 (2); 96 x 96 (2); 256 x 256
+    ("f32", 1, 11162, 130),    # 64 x 64, 32 slices; 64 x 64; 96 x 96
+    ("f32", 9, 69, 3646),      # 64 x 64, 9 slices; 64 x 64; 64 x 64
+    ("f32", 4, 10127, 129),    # 64 x 64 (2), 10 slices; 64 x 64; 192 x 192
+    ("f32", 4, 140, 15184),    # 64 x 64 (2), 10 slices; 64 x 64; 192 x 128
+    ("bf16", 9, 11475, 976),   # 128 x 128, 3 slices; 64 x 64; 192 x 128
+    ("bf16", 2, 987, 6115),    # 128 x 128 (2), 3 slices; 96 x 96; 128 x 128
+    ("bf16", 2, 1469, 7439),   # 192 x 192, 3 slices; 128 x 128 (2); 192 x 128
+    ("bf16", 1, 8977, 2972),   # 256 x 256, 3 slices; 192 x 192; 192 x 192
+    ("bf16", 4, 680, 800),     # 96 x 96; 64 x 64; 64 x 64
+    ("bf16", 4, 646, 1917),    # 96 x 96 (2); 64 x 64; 192 x 128
+    ("bf16", 2, 8356, 513),    # 96 x 96 (2), 6 slices; 64 x 64; 192 x 128
+    ("bf16", 2, 1563, 1538),   # 128 x 128 (2); 128 x 128 (2); 192 x 128
+    ("bf16", 1, 1043, 1123),   # 64 x 64 (2); 64 x 64 (2); 96 x 96
+    ("bf16", 1, 1873, 1604),   # 96 x 96 (2); 96 x 96 (2); 128 x 128 (2)
+    ("bf16", 9, 2850, 65),     # 64 x 64, 9 slices; 64 x 64; 128 x 128
+    ("bf16", 1, 4121, 709),    # 64 x 64 (2), 3 slices; 64 x 64; 128 x 128 (2)
+    ("bf16", 4, 77, 10474),    # 64 x 64, 21 slices; 64 x 64; 192 x 192
+    ("bf16", 9, 6971, 152),    # 64 x 64 (2), 4 slices; 64 x 64; 256 x 256
+    ("bf16", 1, 926, 899),     # 64 x 64; 64 x 64; 64 x 64 (2)
+    ("bf16", 1, 1420, 1293),   # 64 x 64 (2); 64 x 64 (2); 96 x 96 (2)
+    ("bf16", 9, 1309, 650),    # 128 x 128 (2); 64 x 64; 192 x 192
+    ("f32", 9, 1200, 1250),    # 128 x 128; 128 x 128; 256 x 256
+    ("f32", 4, 7483, 1010),    # 128 x 128, 3 slices; 128 x 128 (2); 192 x 128
+    ("f32", 9, 1120, 650),     # 128 x 128 (2); 64 x 64; 192 x 192
+    ("f32", 9, 193, 11889),    # 128 x 128 (2), 9 slices; 64 x 64; 128 x 128
+    ("f32", 2, 1445, 7276),    # 192 x 192, 3 slices; 128 x 128 (2); 192 x 128
+    ("f32", 1, 3035, 4387),    # 256 x 256, 3 slices; 64 x 64; 256 x 256
+    ("f32", 1, 15394, 3),      # 64 x 64 (2), 31 slices; 64 x 64; 64 x 64
+    ("f32", 4, 654, 665),      # 96 x 96 (2); 96 x 96 (2); 64 x 64
+    ("f32", 9, 13104, 130),    # 96 x 96 (2), 9 slices; 64 x 64; 192 x 192
+    ("f32", 4, 1009, 1078),    # 128 x 128 (2); 128 x 128 (2); 192 x 128
+    ("f32", 1, 479, 487),      # 64 x 64 (2); 64 x 64 (2); 64 x 64 (2)
+    ("f32", 2, 66, 12289),     # 64 x 64, 30 slices; 64 x 64; 128 x 128
+    ("f32", 2, 461, 3194),     # 64 x 64 (2), 3 slices; 64 x 64 (2); 128 x 128 (2)
+    ("f32", 4, 8426, 133),     # 64 x 64 (2), 10 slices; 64 x 64; 192 x 192
+    ("f32", 4, 15888, 157),    # 64 x 64 (2), 10 slices; 64 x 64; 256 x 256
+    ("f32", 1, 653, 1650),     # 64 x 64 (2), 3 slices; 64 x 64 (2); 96 x 96 (2)
 ]
 COEF = (3.4445, -4.7750, 2.0315)
 
