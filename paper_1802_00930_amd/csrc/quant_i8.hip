@@ -142,27 +142,27 @@ __global__ __launch_bounds__(kBlock) void k_transpose_i8(const int8_t* __restric
 }
 
 // Column maxima of |x[r][c] roww[r]| and column sums of x over slices of the rows:
-// workgroups of 256 columns by one slice, eight rows at a time.
+// workgroups of 64 columns by one slice, 32 rows at a time.
 template <int T>
 __global__ __launch_bounds__(kBlock) void k_col_max(const typename Elem<T>::type* __restrict__ src, int64_t rows,
                                                     int64_t cols, const float* __restrict__ roww, int64_t slice,
                                                     uint32_t cblocks, uint32_t* __restrict__ pmax,
                                                     float* __restrict__ psum) {
-  __shared__ uint32_t smax[8][256];
-  __shared__ float ssum[8][256];
-  const int cv = threadIdx.x & 31, rg = threadIdx.x >> 5;
-  const int64_t c = (int64_t)(blockIdx.x % cblocks) * 256 + cv * 8, part = blockIdx.x / cblocks;
+  __shared__ __align__(16) uint32_t smax[kBlock / 64][64];
+  __shared__ __align__(16) float ssum[kBlock / 64][64];
+  const int cv = threadIdx.x & 7, rg = threadIdx.x >> 3;
+  const int64_t c0 = (int64_t)(blockIdx.x % cblocks) * 64, c = c0 + cv * 8, part = blockIdx.x / cblocks;
   const int64_t r1 = min(rows, (part + 1) * slice);
   uint32_t mx[8] = {};
   float sum[8] = {};
   constexpr int U = 4;  // rows in flight
-  for (int64_t r = part * slice + rg; r < r1; r += 8 * U) {
+  for (int64_t r = part * slice + rg; r < r1; r += 32 * U) {
     float v[U][8], w[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const bool in = r + u * 8 < r1;
-      w[u] = in ? roww[r + u * 8] : 0.f;
-      load_n<T, 8>(src + (r + u * 8) * cols + c, in ? cols - c : 0, v[u]);
+      const bool in = r + u * 32 < r1;
+      w[u] = in ? roww[r + u * 32] : 0.f;
+      load_n<T, 8>(src + (r + u * 32) * cols + c, in ? cols - c : 0, v[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -172,83 +172,66 @@ __global__ __launch_bounds__(kBlock) void k_col_max(const typename Elem<T>::type
         sum[i] += v[u][i];
       }
   }
+  // over the wave's eight rows, then over the waves
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    smax[rg][cv * 8 + i] = mx[i];
-    ssum[rg][cv * 8 + i] = sum[i];
-  }
-  __syncthreads();
-  const int64_t oc = (int64_t)(blockIdx.x % cblocks) * 256 + threadIdx.x;
-  uint32_t m = 0;
-  float s = 0.f;
+  for (int o = 8; o < 64; o <<= 1)
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    m = max(m, smax[i][threadIdx.x]);
-    s += ssum[i][threadIdx.x];
-  }
-  if (oc < cols) {
-    pmax[part * cols + oc] = m;
-    psum[part * cols + oc] = s;
-  }
-}
-
-// Scales of the columns (and their sums) from the slices: 64 columns a workgroup, its
-// four waves every fourth slice, the waves' results in order.
-__global__ __launch_bounds__(kBlock) void k_col_scale(const uint32_t* __restrict__ pmax, const float* __restrict__ psum,
-                                                      int32_t parts, int64_t cols, float* __restrict__ scale,
-                                                      float* __restrict__ inv, float* __restrict__ sums) {
-  __shared__ uint32_t wm[4][64];
-  __shared__ float wsum[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t c = (int64_t)blockIdx.x * 64 + lane, at = min(c, cols - 1);
-  uint32_t m = 0;
-  float s = 0.f;
-  for (int32_t p = wave; p < parts; p += 32) {  // eight loads in flight
-    uint32_t vm[8];
-    float vs[8];
-#pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      const int64_t o = (int64_t)min(p + u * 4, parts - 1) * cols + at;
-      vm[u] = pmax[o];
-      vs[u] = psum[o];
+    for (int i = 0; i < 8; ++i) {
+      mx[i] = max(mx[i], (uint32_t)__shfl_xor((int)mx[i], o, 64));
+      sum[i] += __shfl_xor(sum[i], o, 64);
     }
+  if ((threadIdx.x & 63) < 8) {
 #pragma unroll
-    for (int u = 0; u < 8; ++u)
-      if (p + u * 4 < parts) {
-        m = max(m, vm[u]);
-        s += vs[u];
-      }
+    for (int i = 0; i < 8; ++i) {
+      smax[threadIdx.x >> 6][cv * 8 + i] = mx[i];
+      ssum[threadIdx.x >> 6][cv * 8 + i] = sum[i];
+    }
   }
-  wm[wave][lane] = m;
-  wsum[wave][lane] = s;
   __syncthreads();
-  if (wave || c >= cols) return;
-  m = max(max(m, wm[1][lane]), max(wm[2][lane], wm[3][lane]));
-  const I8Scale k = i8_scale(m);
-  scale[c] = k.s;
-  inv[c] = k.inv;
-  if (sums) sums[c] = (s + wsum[1][lane]) + (wsum[2][lane] + wsum[3][lane]);
+  const int t = threadIdx.x;
+  if (t < 64 && c0 + t < cols) {
+    pmax[part * cols + c0 + t] = max(max(smax[0][t], smax[1][t]), max(smax[2][t], smax[3][t]));
+    psum[part * cols + c0 + t] = (ssum[0][t] + ssum[1][t]) + (ssum[2][t] + ssum[3][t]);
+  }
 }
 
 // x[r][c] roww[r] rounded by column scale into qt [cols][ldt]: tiles of 128 rows x
-// 64 columns, a thread 4 x 8 of them.
+// 64 columns, a thread 4 x 8 of them.  The columns' scales come from the slices'
+// maxima, at most kMostParts of them, in every tile; the first row of tiles writes them
+// and the columns' sums.
+constexpr int kMostParts = 32;
 template <int T, int MODE>
 __global__ __launch_bounds__(kBlock) void k_col_i8_t(const typename Elem<T>::type* __restrict__ src, int64_t rows,
                                                      int64_t cols, const float* __restrict__ roww,
-                                                     const float* __restrict__ scale,
-                                                     const float* __restrict__ inv, int8_t* __restrict__ qt,
-                                                     int64_t ldt, uint32_t ctiles, uint32_t k0, uint32_t k1,
-                                                     uint32_t role) {
+                                                     const uint32_t* __restrict__ pmax,
+                                                     const float* __restrict__ psum, int32_t parts,
+                                                     float* __restrict__ scale, float* __restrict__ sums,
+                                                     int8_t* __restrict__ qt, int64_t ldt, uint32_t ctiles,
+                                                     uint32_t k0, uint32_t k1, uint32_t role) {
   __shared__ TileT<64> tile;
+  __shared__ __align__(16) float ks[64], ki[64];
+  __shared__ uint32_t wm[kBlock / 64][64];
+  __shared__ float wsum[kBlock / 64][64];
   const int64_t r0 = (int64_t)(blockIdx.x / ctiles) * 128, c0 = (int64_t)(blockIdx.x % ctiles) * 64;
   const int c8 = threadIdx.x & 7, r4 = threadIdx.x >> 3;
   const int64_t c = c0 + c8 * 8;
-  float ks[8], ki[8];
-  load_n<DFP_F32, 8>(scale + c, cols - c, ks);
-  load_n<DFP_F32, 8>(inv + c, cols - c, ki);
-  I8Scale k[8];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t at = min(c0 + lane, cols - 1);
+  uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) k[i] = i8_scale_of(ks[i], ki[i]);
+  for (int i = 0; i < kMostParts / (kBlock / 64); ++i)
+    m = max(m, pmax[(int64_t)min(wave + i * (kBlock / 64), parts - 1) * cols + at]);
+  wm[wave][lane] = m;
+  const bool first = r0 == 0 && sums;
+  if (first) {
+    float p[kMostParts / (kBlock / 64)], s = 0.f;
+#pragma unroll
+    for (int i = 0; i < kMostParts / (kBlock / 64); ++i)
+      p[i] = psum[(int64_t)min(wave + i * (kBlock / 64), parts - 1) * cols + at];
+#pragma unroll
+    for (int i = 0; i < kMostParts / (kBlock / 64); ++i) s += wave + i * (kBlock / 64) < parts ? p[i] : 0.f;
+    wsum[wave][lane] = s;
+  }
   float v[4][8];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -263,6 +246,19 @@ __global__ __launch_bounds__(kBlock) void k_col_i8_t(const typename Elem<T>::typ
       for (int i = 0; i < 8; ++i) v[j][i] = 0.f;
     }
   }
+  __syncthreads();
+  if (wave == 0) {
+    const I8Scale s = i8_scale(max(max(wm[0][lane], wm[1][lane]), max(wm[2][lane], wm[3][lane])));
+    ks[lane] = s.s;
+    ki[lane] = s.inv;
+    if (r0 == 0 && c0 + lane < cols) scale[c0 + lane] = s.s;
+  } else if (wave == 1 && first && c0 + lane < cols) {
+    sums[at] = (wsum[0][lane] + wsum[1][lane]) + (wsum[2][lane] + wsum[3][lane]);
+  }
+  __syncthreads();
+  I8Scale k[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) k[i] = i8_scale_of(ks[c8 * 8 + i], ki[c8 * 8 + i]);
   uint32_t q[4][8];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -328,12 +324,13 @@ dfp_status launch_transpose_i8(const int8_t* q, int64_t rows, int64_t cols, int8
 
 ColPlan plan_cols_i8(int64_t rows, int64_t cols) {
   ColPlan p;
-  const int64_t cb = (cols + 255) / 256;
+  const int64_t cb = (cols + 63) / 64;
   // enough slices for four workgroups a CU, of at least 32 rows
-  int64_t parts = std::max<int64_t>(1, std::min<int64_t>((rows + 31) / 32, 1024 / cb));
+  const int64_t parts =
+      std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>((rows + 31) / 32, kMostParts), 1024 / cb));
   p.slice = (rows + parts - 1) / parts;
   p.parts = (rows + p.slice - 1) / p.slice;
-  p.bytes = (p.parts * 2 + 1) * cols * 4;
+  p.bytes = p.parts * 2 * cols * 4;
   return p;
 }
 
@@ -343,20 +340,17 @@ dfp_status launch_cols_i8_t(int32_t type, int32_t rounding, uint64_t seed, uint3
   const ColPlan p = plan_cols_i8(rows, cols);
   uint32_t* pmax = (uint32_t*)ws;
   float* psum = (float*)(pmax + p.parts * cols);
-  float* inv = psum + p.parts * cols;
-  const uint32_t cb = (uint32_t)((cols + 255) / 256);
   const uint32_t k0 = (uint32_t)seed, k1 = (uint32_t)(seed >> 32);
   const int64_t rt = (rows + 127) / 128, ct = (cols + 63) / 64;
   return with_type(type, [&](auto tc) -> dfp_status {
     constexpr int T = decltype(tc)::value;
     typedef const typename Elem<T>::type* S;
-    DFP_LAUNCH(K_I8_COLS, k_col_max<T>, dim3((unsigned)(cb * p.parts)), dim3(kBlock), 0, st, (S)src, rows, cols, roww,
-               p.slice, cb, pmax, psum);
-    DFP_LAUNCH(K_I8_COLS, k_col_scale, dim3((unsigned)((cols + 63) / 64)), dim3(kBlock), 0, st, pmax, psum,
-               (int32_t)p.parts, cols, scale, inv, sums);
+    DFP_LAUNCH(K_I8_COLS, k_col_max<T>, dim3((unsigned)(ct * p.parts)), dim3(kBlock), 0, st, (S)src, rows, cols, roww,
+               p.slice, (uint32_t)ct, pmax, psum);
     return with_mode(rounding, [&](auto mc) -> dfp_status {
       DFP_LAUNCH(K_I8_COLS, (k_col_i8_t<T, decltype(mc)::value>), dim3((unsigned)(rt * ct)), dim3(kBlock), 0, st,
-                 (S)src, rows, cols, roww, scale, inv, qt, i8_ld(rows), (uint32_t)ct, k0, k1, role);
+                 (S)src, rows, cols, roww, pmax, psum, (int32_t)p.parts, scale, sums, qt, i8_ld(rows),
+                 (uint32_t)ct, k0, k1, role);
       return DFP_OK;
     });
   });

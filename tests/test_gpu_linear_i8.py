@@ -229,6 +229,16 @@ def test_layer(m, n, k, t):
     layer.check()
 
 
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+@pytest.mark.parametrize("m,n,k", [(131071, 3, 2), (30001, 65, 10), (33, 70000, 3), (1025, 4100, 5)])
+def test_long_and_wide_gradients(m, n, k, t):
+    """Columns whose maxima and sums come from many slices of the tokens, or from one."""
+    note("layer %dx%dx%d %s" % (m, n, k, t))
+    layer = Layer(m, n, k, t)
+    layer.run()
+    layer.check()
+
+
 @pytest.mark.parametrize("m,n,k", [(3, 5, 9), (20, 130, 33)])
 def test_layer_stochastic(m, n, k):
     layer = Layer(m, n, k, "bf16", rounding="stochastic", seed=99)
