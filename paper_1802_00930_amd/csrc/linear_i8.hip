@@ -46,6 +46,8 @@ __device__ __forceinline__ void store_quad(const I8Args& g, int64_t i, int64_t j
 }
 
 // SLICED: the tiles of every slice in turn, their sums to g.part.
+// 16384 x 8192 x 8192 BF16 out: 855 to 990 us (2570 to 2220 TOP/s, by how hot the card
+// runs); 4096^3 61 us (2240 TOP/s: one round of tiles that start and end together).
 template <int T, bool SLICED, class Q>
 __global__ __launch_bounds__(Q::kThreads, 2) void k_tiles(I8Args g) {
   typedef typename Q::template Tile<Prod::I8> Tile;
@@ -105,7 +107,8 @@ __global__ __launch_bounds__(Q::kThreads, 2) void k_tiles(I8Args g) {
   }
 }
 
-// The slices' sums, four columns of a row a thread.
+// The slices' sums, four columns of a row a thread: bound by the launch and a trip to
+// memory (4 us), then by the sums' bytes.
 template <int T>
 __global__ __launch_bounds__(256) void k_slices(I8Args g, int32_t slices) {
   const int64_t nq = (g.n + 3) / 4, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -129,13 +132,14 @@ __global__ __launch_bounds__(256) void k_slices(I8Args g, int32_t slices) {
 // Few rows.  A workgroup takes 16 columns of up to 16 RT rows over the whole
 // reduction: its waves deal out the pieces among them, every lane reading 16 bytes
 // of a weight row straight into an MFMA operand (no LDS: nothing is read twice),
-// and their sums meet in LDS.
+// and their sums meet in LDS.  Bound by the latency of the weights' bytes: 16 rows by
+// 4096 x 4096 7.9 us (2.1 TB/s), by 8192 x 8192 19.4 us (3.5 TB/s).
 constexpr int kFewWaves = 8;
 constexpr int kTokenRows = 2;
 constexpr int kTokenVecs = 8;                                        // of 8 elements, a lane's share of a row
 constexpr int kTokenBytes = 64 * 8 * kTokenVecs * kFewWaves + 16 * kTokenRows;  // all waves' rows, and their padding
 // log2 of the waves that share a row of x
-__host__ __device__ __forceinline__ int32_t token_shift(int64_t m) { return m == 1 ? 3 : m == 2 ? 2 : m <= 4 ? 1 : 0; }
+__host__ __device__ __forceinline__ int32_t token_shift(int64_t m) { return m == 1 ? 3 : 2; }
 template <int T, int RT, int UNROLL>
 __global__ __launch_bounds__(64 * kFewWaves) void k_few(I8Args g) {
   __shared__ int32_t part[kFewWaves][RT * 256];
@@ -185,7 +189,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few(I8Args g) {
 
 // One token or a few, quantised on the way: every workgroup of k_few's kind turns
 // the rows of x into INT8 in its own LDS, which takes the launch of a quantiser out
-// of the call.  The first pieces of the weights are requested before.
+// of the call.  The first pieces of the weights are requested before.  One row by
+// 4096 x 4096: 7.2 us (16.8 MB, 2.3 TB/s), in two launches 10.9.
 template <int T, int MODE, int UNROLL>
 __global__ __launch_bounds__(64 * kFewWaves) void k_token(I8Args g, const typename Elem<T>::type* __restrict__ x,
                                                           int32_t k, uint32_t k0, uint32_t k1) {
@@ -207,7 +212,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_token(I8Args g, const typena
         b[u][h] = *(const mv4i*)(pb + (int64_t)min(p + u * kFewWaves, pieces - 1) * kPiece + h * 64);
   };
   fetch(wave);
-  // 8, 4, 2 or 1 waves a row; the row stays in registers
+  // eight or four waves a row; the row stays in registers
   const int32_t sh = token_shift(g.m), row = wave >> sh, sub = wave & ((1 << sh) - 1);
   float v[kTokenVecs][8];
   uint32_t mx = 0;
@@ -272,9 +277,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_token(I8Args g, const typena
 //   k_tiles  tile_us; with weights that come from memory, as they do for few rows, a
 //            quarter more.  Slices mean that their sums are written and read (4 TB/s)
 //            and a second kernel (4).
-// At 64 rows: 4096 x 4096 k_few 13.8, tiles 12.7; 8192 x 2048 13.4 and 9.2; 8192 x
-// 8192 44 and 22; 1024 x 1024 5.0 and 5.2.  At 24: 9.6 and 13.6; 8.5 and 8.8; 25.5 and
-// 18.8; 3.6 and 4.8.
+// At 64 rows: 4096 x 4096 k_few 13.8, tiles 12.0; 8192 x 2048 13.4 and 8.2; 8192 x
+// 8192 44.7 and 22.1; 1024 x 1024 5.0 and 5.1.  At 24: 9.7 and 10.0; 8.6 and 7.3; 25.4 and
+// 20.4; 3.5 and 4.7.  At 16, where k_few runs always: 7.9 and 9.7; 7.0 and 7.0; 19.4 and
+// 20.3; 3.2 and 4.5.
 constexpr int32_t kFewRows = 64;
 constexpr int64_t kMostPartBytes = 64 << 20;
 

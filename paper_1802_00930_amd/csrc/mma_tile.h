@@ -60,11 +60,14 @@ typedef __attribute__((address_space(3))) void* mma_lds_t;
 // are permuted by an XOR with three bits of the row, at the source address since
 // the LDS side of such a load is linear: row bits 0 - 2 for A, 0, 1 and 3 for B,
 // which differ in the eight rows that are read at once: no bank conflicts.
-// 8192 x 8192 outputs, 8192 bytes a row, 256 x 256 tiles by 4 x 2 waves: I8 2350
-// TOP/s, F16 1180 TFLOP/s, F16X2 1440 (its 3 products; the MFMAs run 54 and 68 % of
-// the cycles, at 2.07 GHz).  Staging through registers reaches 2240, 1110 and 1210,
-// 128 x 128 outputs a wave (one wave a SIMD) 1840; two groups of waves that
-// take turns between reads and MFMAs, four barriers a piece, 2070.
+// 8192 x 8192 outputs, 8192 bytes a row, 256 x 256 tiles by 4 x 2 waves: I8 480 us,
+// 2290 TOP/s (library 2331), F16 486 us, 1130 TFLOP/s (1483), F16X2 600 us, 1380 of its 3
+// products, by card 4 % either way.  The MFMAs run 54 and 68 % of the cycles; LDS
+// is half idle.  A part of that is the card's power: operands of zeros take 424, 422
+// and 480 us.  Left: staging through registers (2240, 1110 and 1210), 128 x 128 outputs a
+// wave, one wave a SIMD, the next half's reads between this half's MFMAs (2230, 1100 and
+// 1370), two groups of waves that take turns between reads and MFMAs, four barriers a
+// piece (I8 2070), 32 x 32 MFMAs and deeper rings (no gain).
 //
 // KG > 1: as many groups of WM x WN waves take the pieces in turn, each with a ring of
 // its own, and group 0 ends with the sums of all: for a CU that has one tile, where a
