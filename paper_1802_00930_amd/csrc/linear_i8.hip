@@ -76,33 +76,45 @@ __global__ __launch_bounds__(Q::kThreads, 2) void k_tiles(I8Args g) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t i1 = i0 + (wave / WN) * (TM / WM) + (lane & 15);
   const int64_t j1 = j0 + (wave % WN) * (TN / WN) + (lane >> 4) * 8;
+  // 64 or 96 columns of a row one after the other: of 16-bit outputs a store is half a
+  // line, and a tile's lines leave L2 before a half that comes later joins them
+  constexpr int JN = Tile::FN % 4 == 0 ? 4 : Tile::FN % 6 == 0 ? 6 : 2;
 #pragma unroll
-  for (int j = 0; j < Tile::FN; j += 2) {
-    const int64_t jj = j1 + j * 16;
-    float sb[8], bias[8];
+  for (int j = 0; j < Tile::FN; j += JN) {
+    float sb[JN / 2][8], bias[JN / 2][8];
     if (!SLICED) {
 #pragma unroll
-      for (int r = 0; r < 8; ++r) sb[r] = fb[jj - j0 + r], bias[r] = fbias[jj - j0 + r];
+      for (int h = 0; h < JN / 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          const int64_t c = j1 - j0 + (j + 2 * h) * 16 + r;
+          sb[h][r] = fb[c], bias[h][r] = fbias[c];
+        }
     }
 #pragma unroll
     for (int i = 0; i < Tile::FM; ++i) {
       const int64_t ii = i1 + i * 16;
-      if (ii >= g.m || jj >= g.n) continue;
-      float v[8];
+      if (ii >= g.m) continue;
 #pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        const int32_t s = acc[i][j + (r >> 2)][r & 3];
-        if (SLICED) {
-          v[r] = __int_as_float(s);  // stored as it is
-        } else {
-          v[r] = (float)s * fa[ii - i0] * sb[r];
-          if (g.bias) v[r] = v[r] + bias[r];
+      for (int h = 0; h < JN / 2; ++h) {
+        const int64_t jj = j1 + (j + 2 * h) * 16;
+        if (jj >= g.n) continue;
+        float v[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          const int32_t s = acc[i][j + 2 * h + (r >> 2)][r & 3];
+          if (SLICED) {
+            v[r] = __int_as_float(s);  // stored as it is
+          } else {
+            v[r] = (float)s * fa[ii - i0] * sb[h][r];
+            if (g.bias) v[r] = v[r] + bias[h][r];
+          }
         }
+        if (SLICED)
+          store_n<DFP_F32, 8>((float*)g.part + ((int64_t)slice * g.m + ii) * g.n + jj, g.n - jj, v);
+        else
+          store_n<T, 8>((typename Elem<T>::type*)g.out + ii * g.n + jj, g.n - jj, v);
       }
-      if (SLICED)
-        store_n<DFP_F32, 8>((float*)g.part + ((int64_t)slice * g.m + ii) * g.n + jj, g.n - jj, v);
-      else
-        store_n<T, 8>((typename Elem<T>::type*)g.out + ii * g.n + jj, g.n - jj, v);
     }
   }
 }
