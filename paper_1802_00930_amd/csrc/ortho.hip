@@ -20,9 +20,10 @@
 // polynomials of A: they commute, and their products are symmetric), and
 // X = P_2 P_1 X = q X + Q X with q = a_2 a_1, Q = a_2 B_1 + a_1 B_2 + B_2 B_1.  That replaces a
 // Gram product and a step by three products of the small side.  An error of A grows by
-// a^2 an iteration, so no more than a^2 a'^2 <= 150 (two such for a = 3.44) are taken
-// before A is computed from X again: 2 to 3 times the error of single iterations, of an
-// update that enters FP32 weights times lr.
+// the square of P's norm an iteration, m = a^2 where a is the largest that a + b s + c s^2
+// gets on [0, 1], so no more than m m' <= 150 (two such for a = 3.44) are taken before A is
+// computed from X again: 2 to 3 times the error of single iterations, of an update that
+// enters FP32 weights times lr.
 //
 // Units: X in 2^-12, A in 2^-10, B in 2^-sb so that |b A + c A A| <= 32768 in it for
 // singular values up to sqrt(2).
@@ -567,6 +568,14 @@ dfp_status launch_mm(int32_t id, const MmPlan& p, int32_t batch, MmArgs& g, hipS
   });
 }
 
+// Largest |a + b s + c s^2| on [0, 1]: at an end or at the vertex.
+double most_of(double a, double b, double c) {
+  double m = std::max(std::fabs(a), std::fabs(a + b + c));
+  const double s = c != 0. ? -b / (2. * c) : 0.;
+  if (s > 0. && s < 1.) m = std::max(m, std::fabs(a + s * (b + s * c)));
+  return m;
+}
+
 // Largest unit, 2^12 at most, that keeps an operand of up to `most` at 32768 or less.
 float unit_for(double most) {
   int s = 12;
@@ -650,7 +659,8 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
         q = qq[k & 1], uq = un;
       }
       qa *= ca;
-      grown *= (double)ca * ca;
+      const double most = most_of(ca, cb, cc);
+      grown *= most * most;
       if (!MUON || !p.grouped || s + 1 >= d.steps || grown > 150.) break;
       // A = P A P
       const float ua = (float)(1 << kUnitA);

@@ -175,7 +175,9 @@ SCHEDULES = {
     # coefficients of their own for each step, the first far above the others: within [0, 2] on [0, 1]
     "falling": [(8.287, -23.596, 17.300), (4.107, -2.948, 0.545), (3.949, -2.909, 0.552), (3.318, -2.488, 0.510),
                 (2.301, -1.669, 0.419)],
-    # the same rounded further: from 1 they end above 1000, past the documented range (4)
+    # the middle of [0, 1] grows most
+    "middle": [(1.2, 0.3, -0.5)] * 8,
+    # "falling" rounded further: from 1 they end above 1000, past the documented range (4)
     "out of range": [(8.2, -23.0, 17.0), (4.1, -2.9, 0.55), (3.9, -2.8, 0.55), (3.3, -2.4, 0.5), (2.0, -1.5, 0.5)],
 }
 
