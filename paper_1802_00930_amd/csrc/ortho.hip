@@ -596,7 +596,7 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
   double* part = (double*)(base + p.norm);
   const unsigned nb = (unsigned)d.batch;
   const int64_t n = p.R * p.C;
-  const int32_t parts = (int32_t)std::min<int64_t>(n < (1 << 23) ? kBlock : kNormParts, (n + kBlock * 4 - 1) / (kBlock * 4));
+  const int32_t parts = (int32_t)std::min<int64_t>(n < (1 << 23) ? kBlock : kNormParts, (n + kBlock * 16 - 1) / (kBlock * 16));
   DFP_LAUNCH(K_ORTHO_NORM, (k_norm<T, MUON>), dim3((unsigned)parts, nb), dim3(kBlock), 0, st, src, n, part);
   // gram: the longer side contiguous
   uint8_t* rowop = p.tall ? step[0] : gram;
