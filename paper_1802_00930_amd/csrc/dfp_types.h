@@ -28,16 +28,42 @@ struct Elem<DFP_F16> {
 
 inline int64_t type_bytes(int32_t type) { return type == DFP_F32 ? 4 : 2; }
 
-// N elements from p (aligned to an element only; the vector loads of gfx950 take that).
+// N elements as they lie in memory, from p on (aligned to an element only; the vector
+// loads of gfx950 take that).  Loaded first and turned into numbers behind all
+// loads of a loop: fetch_n is a branch, and what uses the elements in it waits for
+// them there (16384 x 8192 BF16 by rows 85.5 us, 72.6 so; 8192 x 2048
+// FP32 19.0 and 16.7).
 template <int T, int N>
-__device__ __forceinline__ void load_n(const typename Elem<T>::type* p, float (&v)[N]) {
-  typedef typename Elem<T>::type E;
-  struct __attribute__((packed, aligned(sizeof(E)))) Raw {
-    E e[N];
-  };
-  const Raw r = *reinterpret_cast<const Raw*>(p);
+struct __attribute__((packed, aligned(sizeof(typename Elem<T>::type)))) Raw {
+  uint32_t w[N * sizeof(typename Elem<T>::type) / 4];
+};
+// The first `have` of N elements, zero behind them.
+template <int T, int N>
+__device__ __forceinline__ void fetch_n(const typename Elem<T>::type* p, int64_t have, Raw<T, N>& r) {
+  constexpr int E = sizeof(typename Elem<T>::type);
 #pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = Elem<T>::up(r.e[i]);
+  for (int i = 0; i < N * E / 4; ++i) r.w[i] = 0u;
+  if (have >= N) {
+    r = *reinterpret_cast<const Raw<T, N>*>(p);
+  } else if (have > 0) {
+#pragma unroll
+    for (int i = 0; i < N * E / 4; ++i) {
+      if constexpr (E == 4)
+        r.w[i] = i < have ? __float_as_uint(p[i]) : 0u;
+      else
+        r.w[i] = (2 * i < have ? (uint32_t)p[2 * i] : 0u) | (2 * i + 1 < have ? (uint32_t)p[2 * i + 1] << 16 : 0u);
+    }
+  }
+}
+template <int T, int N>
+__device__ __forceinline__ void up_n(const Raw<T, N>& r, float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if constexpr (sizeof(typename Elem<T>::type) == 4)
+      v[i] = __uint_as_float(r.w[i]);
+    else
+      v[i] = Elem<T>::up((uint16_t)(r.w[i / 2] >> (i % 2 * 16)));
+  }
 }
 template <int T, int N>
 __device__ __forceinline__ void store_n(typename Elem<T>::type* p, const float (&v)[N]) {
@@ -49,12 +75,11 @@ __device__ __forceinline__ void store_n(typename Elem<T>::type* p, const float (
   for (int i = 0; i < N; ++i) r.e[i] = Elem<T>::down(v[i]);
   *reinterpret_cast<Raw*>(p) = r;
 }
-// The first `have` of N elements, zero behind them.
 template <int T, int N>
 __device__ __forceinline__ void load_n(const typename Elem<T>::type* p, int64_t have, float (&v)[N]) {
-  if (have >= N) return load_n<T, N>(p, v);
-#pragma unroll
-  for (int i = 0; i < N; ++i) v[i] = i < have ? Elem<T>::up(p[i]) : 0.f;
+  Raw<T, N> r;
+  fetch_n<T, N>(p, have, r);
+  up_n<T, N>(r, v);
 }
 template <int T, int N>
 __device__ __forceinline__ void store_n(typename Elem<T>::type* p, int64_t have, const float (&v)[N]) {

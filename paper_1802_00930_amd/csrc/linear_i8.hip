@@ -226,18 +226,16 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_token(I8Args g, const typena
   fetch(wave);
   // eight or four waves a row; the row stays in registers
   const int32_t sh = token_shift(g.m), row = wave >> sh, sub = wave & ((1 << sh) - 1);
+  Raw<T, 8> raw[kTokenVecs];
   float v[kTokenVecs][8];
   uint32_t mx = 0;
 #pragma unroll
   for (int i = 0; i < kTokenVecs; ++i) {
     const int32_t c = ((i << sh | sub) * 64 + lane) * 8;
-    if (row < g.m && c < k) {
-      load_n<T, 8>(x + (int64_t)row * k + c, k - c, v[i]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[i][e] = 0.f;
-    }
+    fetch_n<T, 8>(x + (int64_t)row * k + c, row < g.m ? k - c : 0, raw[i]);
   }
+#pragma unroll
+  for (int i = 0; i < kTokenVecs; ++i) up_n<T, 8>(raw[i], v[i]);
 #pragma unroll
   for (int i = 0; i < kTokenVecs; ++i)
 #pragma unroll

@@ -196,12 +196,14 @@ struct Source {
   float mu;
   bool nesterov;
 };
+// (its elements fetched before, g and the new v)
 template <int T, bool MUON>
-__device__ __forceinline__ void direction(const Source<T>& s, int64_t at, int64_t have, float (&u)[4]) {
-  load_n<T, 4>(s.x + at, have, u);
+__device__ __forceinline__ void direction(const Source<T>& s, const Raw<T, 4>& g, const Raw<DFP_F32, 4>& vnew,
+                                          float (&u)[4]) {
+  up_n<T, 4>(g, u);
   if (MUON) {
     float v[4];
-    load_n<DFP_F32, 4>(s.v + at, have, v);
+    up_n<DFP_F32, 4>(vnew, v);
 #pragma unroll
     for (int i = 0; i < 4; ++i) u[i] = s.nesterov ? fmaf(s.mu, v[i], u[i]) : v[i];
   }
@@ -216,12 +218,19 @@ __global__ __launch_bounds__(kBlock) void k_norm(Source<T> s, int64_t n, double*
   double sum = 0.;
   constexpr int U = 4;  // quads in flight
   for (int64_t i = ((int64_t)blockIdx.x * kBlock + threadIdx.x) * 4; i < n; i += stride * U) {
-    float g[U][4], v[U][4];
+    Raw<T, 4> raw[U];
+    Raw<DFP_F32, 4> old[MUON ? U : 1];
 #pragma unroll
     for (int k = 0; k < U; ++k) {
       const int64_t at = i + k * stride;
-      load_n<T, 4>(s.x + base + at, n - at, g[k]);
-      if (MUON) load_n<DFP_F32, 4>(s.v + base + at, n - at, v[k]);
+      fetch_n<T, 4>(s.x + base + at, n - at, raw[k]);
+      if (MUON) fetch_n<DFP_F32, 4>(s.v + base + at, n - at, old[k]);
+    }
+    float g[U][4], v[U][4];
+#pragma unroll
+    for (int k = 0; k < U; ++k) {
+      up_n<T, 4>(raw[k], g[k]);
+      if (MUON) up_n<DFP_F32, 4>(old[k], v[k]);
     }
 #pragma unroll
     for (int k = 0; k < U; ++k) {
@@ -267,13 +276,17 @@ __global__ __launch_bounds__(kBlock) void k_pack(Source<T> s, int64_t R, int64_t
     const int32_t at = threadIdx.x + i * kBlock;
     sums[i] = at < parts ? part[b * parts + at] : 0.;
   }
-  float u[4][4];
+  Raw<T, 4> raw[4];
+  Raw<DFP_F32, 4> vnew[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int64_t r = r0 + (threadIdx.x >> 4) + i * 16, c = c0 + cc;
-    u[i][0] = u[i][1] = u[i][2] = u[i][3] = 0.f;
-    if (r < R && c < C) direction<T, MUON>(s, (b * R + r) * C + c, C - c, u[i]);
+    const int64_t r = r0 + (threadIdx.x >> 4) + i * 16, c = c0 + cc, at = (b * R + r) * C + c;
+    fetch_n<T, 4>(s.x + at, r < R ? C - c : 0, raw[i]);
+    if (MUON) fetch_n<DFP_F32, 4>(s.v + at, r < R ? C - c : 0, vnew[i]);
   }
+  float u[4][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) direction<T, MUON>(s, raw[i], vnew[i], u[i]);
   double sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
@@ -380,7 +393,7 @@ __device__ __forceinline__ void finish(const MmArgs& g, int64_t b, int64_t i0, i
     if (KIND == LAST && MUON && i < g.R && j < g.C) load_n<DFP_F32, 8>(g.w + (b * g.R + i) * g.C + j, g.C - j, w[fi]);
   }
   float dc[8] = {};
-  if (XSTEP && ONE && g.diag_cols && in_n) load_n<DFP_F32, 8>(g.diag + b * g.rp + j, dc);
+  if (XSTEP && ONE && g.diag_cols && in_n) load_n<DFP_F32, 8>(g.diag + b * g.rp + j, 8, dc);
 #pragma unroll
   for (int fi = 0; fi < FM; ++fi) {
     const int64_t i = i1 + fi * 16;

@@ -42,13 +42,19 @@ __global__ __launch_bounds__(kBlock) void k_rows_i8(const typename Elem<T>::type
     const int64_t r = min(r0 + threadIdx.x / G, rows - 1);
     const bool mine = r0 + threadIdx.x / G < rows;
     const typename Elem<T>::type* x = src + r * cols;
-    auto load = [&](int64_t c, float (&v)[8]) {
-      load_n<T, 8>(x + c, cols - c, v);
+    Raw<T, 8> raw[NV > 0 ? NV : 1];
+    Raw<DFP_F32, 8> weight[NV > 0 && WEIGHTED ? NV : 1];
+    auto fetch = [&](int64_t c, int i) {
+      fetch_n<T, 8>(x + c, cols - c, raw[i]);
+      if (WEIGHTED) fetch_n<DFP_F32, 8>(colw + c, cols - c, weight[i]);
+    };
+    auto number = [&](int i, float (&v)[8]) {
+      up_n<T, 8>(raw[i], v);
       if (WEIGHTED) {
         float w[8];
-        load_n<DFP_F32, 8>(colw + c, cols - c, w);
+        up_n<DFP_F32, 8>(weight[i], w);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= w[i];
+        for (int e = 0; e < 8; ++e) v[e] *= w[e];
       }
     };
     uint32_t mx = 0;
@@ -59,12 +65,16 @@ __global__ __launch_bounds__(kBlock) void k_rows_i8(const typename Elem<T>::type
     float v[NV > 0 ? NV : 1][8];
     if constexpr (NV > 0) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) load(((int64_t)t + i * G) * 8, v[i]);
+      for (int i = 0; i < NV; ++i) fetch(((int64_t)t + i * G) * 8, i);
 #pragma unroll
-      for (int i = 0; i < NV; ++i) maxof(v[i]);
+      for (int i = 0; i < NV; ++i) {
+        number(i, v[i]);
+        maxof(v[i]);
+      }
     } else {
       for (int64_t c = t; c < nvec; c += G) {
-        load(c * 8, v[0]);
+        fetch(c * 8, 0);
+        number(0, v[0]);
         maxof(v[0]);
       }
     }
@@ -88,7 +98,8 @@ __global__ __launch_bounds__(kBlock) void k_rows_i8(const typename Elem<T>::type
       }
     } else {
       for (int64_t c = t; c < nvec; c += G) {
-        load(c * 8, v[0]);
+        fetch(c * 8, 0);
+        number(0, v[0]);
         if (mine)
           *reinterpret_cast<uint2*>(q + r * ld + c * 8) = i8_round8<MODE>(v[0], k, r * cols + c * 8, k0, k1, role);
       }
@@ -163,20 +174,24 @@ __global__ __launch_bounds__(kBlock) void k_col_max(const typename Elem<T>::type
   float sum[8] = {};
   constexpr int U = 4;  // rows in flight
   for (int64_t r = part * slice + rg; r < r1; r += 32 * U) {
-    float v[U][8], w[U];
+    Raw<T, 8> raw[U];
+    float w[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const bool in = r + u * 32 < r1;
       w[u] = in ? roww[r + u * 32] : 0.f;
-      load_n<T, 8>(src + (r + u * 32) * cols + c, in ? cols - c : 0, v[u]);
+      fetch_n<T, 8>(src + (r + u * 32) * cols + c, in ? cols - c : 0, raw[u]);
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u) {
+      float v[8];
+      up_n<T, 8>(raw[u], v);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        mx[i] = max(mx[i], __float_as_uint(v[u][i] * w[u]) & 0x7fffffffu);
-        sum[i] += v[u][i];
+        mx[i] = max(mx[i], __float_as_uint(v[i] * w[u]) & 0x7fffffffu);
+        sum[i] += v[i];
       }
+    }
   }
   // over the wave's eight rows, then over the waves
 #pragma unroll
@@ -239,19 +254,19 @@ __global__ __launch_bounds__(kBlock) void k_col_i8_t(const typename Elem<T>::typ
     for (int i = 0; i < kMostParts / (kBlock / 64); ++i) s += wave + i * (kBlock / 64) < parts ? p[i] : 0.f;
     wsum[wave][lane] = s;
   }
-  float v[4][8];
+  Raw<T, 8> raw[4];
+  float v[4][8], weight[4];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const int64_t r = r0 + r4 * 4 + j;
-    if (r < rows && c < cols) {
-      load_n<T, 8>(src + r * cols + c, cols - c, v[j]);
-      const float w = roww[r];
+    weight[j] = r < rows ? roww[r] : 0.f;
+    fetch_n<T, 8>(src + r * cols + c, r < rows ? cols - c : 0, raw[j]);
+  }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[j][i] *= w;
-    } else {
+  for (int j = 0; j < 4; ++j) {
+    up_n<T, 8>(raw[j], v[j]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[j][i] = 0.f;
-    }
+    for (int i = 0; i < 8; ++i) v[j][i] *= weight[j];
   }
   __syncthreads();
   if (wave == 0) {
