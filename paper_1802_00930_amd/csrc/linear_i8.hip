@@ -201,10 +201,13 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few(I8Args g) {
 
 // One token or a few, quantised on the way: every workgroup of k_few's kind turns
 // the rows of x into INT8 in its own LDS, which takes the launch of a quantiser out
-// of the call.  The first pieces of the weights are requested before.  One row by
-// 4096 x 4096: 7.2 us (16.8 MB, 2.3 TB/s), in two launches 10.9.
+// of the call.  The first pieces of the weights are on their way meanwhile, requested
+// after the row, since loads are waited for in order (one row by 4096 x 4096 7.4 us, 2.3
+// TB/s; before the row 8.4, in two launches 10.9).  The row stays packed, in 128 registers
+// with all else, so that two workgroups share a CU (one row by 8192 x 8192: 16.2 us,
+// with one 19.3).
 template <int T, int MODE, int UNROLL>
-__global__ __launch_bounds__(64 * kFewWaves) void k_token(I8Args g, const typename Elem<T>::type* __restrict__ x,
+__global__ __launch_bounds__(64 * kFewWaves, 4) void k_token(I8Args g, const typename Elem<T>::type* __restrict__ x,
                                                           int32_t k, uint32_t k0, uint32_t k1) {
   __shared__ __align__(16) uint8_t xq[kTokenBytes];
   __shared__ int32_t part[kFewWaves][256];
@@ -223,23 +226,23 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_token(I8Args g, const typena
       for (int h = 0; h < 2; ++h)
         b[u][h] = *(const mv4i*)(pb + (int64_t)min(p + u * kFewWaves, pieces - 1) * kPiece + h * 64);
   };
-  fetch(wave);
   // eight or four waves a row; the row stays in registers
   const int32_t sh = token_shift(g.m), row = wave >> sh, sub = wave & ((1 << sh) - 1);
   Raw<T, 8> raw[kTokenVecs];
-  float v[kTokenVecs][8];
   uint32_t mx = 0;
 #pragma unroll
   for (int i = 0; i < kTokenVecs; ++i) {
     const int32_t c = ((i << sh | sub) * 64 + lane) * 8;
     fetch_n<T, 8>(x + (int64_t)row * k + c, row < g.m ? k - c : 0, raw[i]);
   }
+  fetch(wave);
 #pragma unroll
-  for (int i = 0; i < kTokenVecs; ++i) up_n<T, 8>(raw[i], v[i]);
+  for (int i = 0; i < kTokenVecs; ++i) {
+    float v[8];
+    up_n<T, 8>(raw[i], v);
 #pragma unroll
-  for (int i = 0; i < kTokenVecs; ++i)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) mx = max(mx, __float_as_uint(v[i][e]) & 0x7fffffffu);
+    for (int e = 0; e < 8; ++e) mx = max(mx, __float_as_uint(v[e]) & 0x7fffffffu);
+  }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) mx = max(mx, (uint32_t)__shfl_xor((int)mx, o, 64));
   if (lane == 0) red[wave] = mx;
@@ -250,8 +253,10 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_token(I8Args g, const typena
 #pragma unroll
   for (int i = 0; i < kTokenVecs; ++i) {
     const int32_t c = ((i << sh | sub) * 64 + lane) * 8;
+    float v[8];
+    up_n<T, 8>(raw[i], v);
     if (row < g.m && c < (int32_t)g.ld)
-      *(uint2*)(xq + row * stride + c) = i8_round8<MODE>(v[i], sc, (int64_t)row * k + c, k0, k1, DFP_ROLE_X);
+      *(uint2*)(xq + row * stride + c) = i8_round8<MODE>(v, sc, (int64_t)row * k + c, k0, k1, DFP_ROLE_X);
   }
   __syncthreads();
   const uint8_t* pa = xq + min(lane & 15, g.m - 1) * stride + (lane >> 4) * 16;
