@@ -361,39 +361,53 @@ __device__ __forceinline__ void mm_tile(const MmArgs& g, uint32_t id, uint32_t* 
     tile_of(id, g.tm, g.tn, 8, im, in);
 }
 
-// What becomes of a wave's sums at 16 FM rows from i0 by 32 columns from j0 (a lane:
-// rows i0 + 16 fi + lane % 16, columns j0 + 8 (lane / 16) ..).  The transposed operand
+// What a wave needs from memory for its sums at 16 FM rows from i0 by 32 columns from
+// j0 (a lane: rows i0 + 16 fi + lane % 16, columns j0 + 8 (lane / 16) ..), all of it
+// requested before the first is used.
+template <int FM>
+struct Old {
+  uint4 hi[FM], lo[FM];
+  float w[FM][8], dg[FM], dc[8];
+};
+template <Prod P, int KIND, bool MUON, int FM>
+__device__ __forceinline__ void fetch_old(const MmArgs& g, int64_t b, int64_t i0, int64_t j0, Old<FM>& o) {
+  constexpr bool ONE = P == Prod::F16, XSTEP = KIND == STEP || KIND == LAST;
+  const int lane = threadIdx.x & 63;
+  const int64_t j = j0 + (lane >> 4) * 8, i1 = i0 + (lane & 15);
+  const bool in_n = j < g.n;
+#pragma unroll
+  for (int fi = 0; fi < FM; ++fi) {
+    const int64_t i = i1 + fi * 16;
+    o.hi[fi] = o.lo[fi] = make_uint4(0, 0, 0, 0);
+    o.dg[fi] = 0.f;
+    if (i >= g.m || !in_n) continue;
+    if (KIND == POLY || XSTEP) {
+      const uint4* d = (const uint4*)(g.old + b * g.sr + i * g.ldr + op_off<P>(j));
+      o.hi[fi] = d[0];
+      if (!ONE) o.lo[fi] = d[4];
+      if (XSTEP && ONE) o.lo[fi] = *(const uint4*)(g.xlo + (b * g.m + i) * (int64_t)g.n + j);
+    }
+    if (XSTEP && ONE && !g.diag_cols) o.dg[fi] = g.diag[b * g.rp + i];
+    if (KIND == LAST && MUON && i < g.R && j < g.C)
+      load_n<DFP_F32, 8>(g.w + (b * g.R + i) * g.C + j, g.C - j, o.w[fi]);
+  }
+#pragma unroll
+  for (int r = 0; r < 8; ++r) o.dc[r] = 0.f;
+  if (XSTEP && ONE && g.diag_cols && in_n) load_n<DFP_F32, 8>(g.diag + b * g.rp + j, 8, o.dc);
+}
+
+// What becomes of those sums.  The transposed operand
 // goes through LDS (`lds`: 32 columns of 16 FM + 8 numbers, this wave's own) so that it
 // is stored in 16-byte runs too: stored from the lanes, two bytes at a time,
 // 2048 x 8192's STEP took 217 us.
 template <Prod P, int KIND, int T, bool MUON, int FM>
 __device__ __forceinline__ void finish(const MmArgs& g, int64_t b, int64_t i0, int64_t j0, bool mirror, uint16_t* lds,
-                                       float (&s)[FM][8]) {
+                                       float (&s)[FM][8], Old<FM>& o) {
   constexpr int kRows = 16 * FM, kStride = kRows + 8;
   constexpr bool ONE = P == Prod::F16, XSTEP = KIND == STEP || KIND == LAST;
   const int lane = threadIdx.x & 63;
   const int64_t j = j0 + (lane >> 4) * 8, i1 = i0 + (lane & 15);
   const bool in_n = j < g.n;
-  // what the rows need from memory, all of it before the first is used
-  uint4 hi[FM], lo[FM];
-  float w[FM][8], dg[FM];
-#pragma unroll
-  for (int fi = 0; fi < FM; ++fi) {
-    const int64_t i = i1 + fi * 16;
-    hi[fi] = lo[fi] = make_uint4(0, 0, 0, 0);
-    dg[fi] = 0.f;
-    if (i >= g.m || !in_n) continue;
-    if (KIND == POLY || XSTEP) {
-      const uint4* d = (const uint4*)(g.old + b * g.sr + i * g.ldr + op_off<P>(j));
-      hi[fi] = d[0];
-      if (!ONE) lo[fi] = d[4];
-      if (XSTEP && ONE) lo[fi] = *(const uint4*)(g.xlo + (b * g.m + i) * (int64_t)g.n + j);
-    }
-    if (XSTEP && ONE && !g.diag_cols) dg[fi] = g.diag[b * g.rp + i];
-    if (KIND == LAST && MUON && i < g.R && j < g.C) load_n<DFP_F32, 8>(g.w + (b * g.R + i) * g.C + j, g.C - j, w[fi]);
-  }
-  float dc[8] = {};
-  if (XSTEP && ONE && g.diag_cols && in_n) load_n<DFP_F32, 8>(g.diag + b * g.rp + j, 8, dc);
 #pragma unroll
   for (int fi = 0; fi < FM; ++fi) {
     const int64_t i = i1 + fi * 16;
@@ -402,7 +416,7 @@ __device__ __forceinline__ void finish(const MmArgs& g, int64_t b, int64_t i0, i
 #pragma unroll
     for (int r = 0; r < 8; ++r) v[r] *= g.unit;
     float x[8];
-    if (KIND == POLY || XSTEP) unpack8(hi[fi], lo[fi], x);
+    if (KIND == POLY || XSTEP) unpack8(o.hi[fi], o.lo[fi], x);
     if (KIND == POLY && !ONE && g.old2) {
       const uint4* d = (const uint4*)(g.old2 + b * g.sr + i * g.ldr + op_off<P>(j));
       float y[8];
@@ -423,15 +437,15 @@ __device__ __forceinline__ void finish(const MmArgs& g, int64_t b, int64_t i0, i
     if (XSTEP) {
 #pragma unroll
       for (int r = 0; r < 8; ++r)
-        v[r] = fmaf(ONE ? (g.diag_cols ? dc[r] : dg[fi]) : g.ca, x[r] * (1.f / (1 << kUnitX)), v[r]);
+        v[r] = fmaf(ONE ? (g.diag_cols ? o.dc[r] : o.dg[fi]) : g.ca, x[r] * (1.f / (1 << kUnitX)), v[r]);
     }
     if (KIND == LAST) {
       if (i >= g.R || j >= g.C) continue;
       const int64_t at = (b * g.R + i) * g.C + j;
       if (MUON) {
 #pragma unroll
-        for (int r = 0; r < 8; ++r) w[fi][r] = fmaf(-g.alpha, v[r], g.keep * w[fi][r]);
-        store_n<DFP_F32, 8>(g.w + at, g.C - j, w[fi]);
+        for (int r = 0; r < 8; ++r) o.w[fi][r] = fmaf(-g.alpha, v[r], g.keep * o.w[fi][r]);
+        store_n<DFP_F32, 8>(g.w + at, g.C - j, o.w[fi]);
       } else {
         store_n<T, 8>((typename Elem<T>::type*)g.out + at, g.C - j, v);
       }
@@ -469,8 +483,8 @@ __device__ __forceinline__ void finish(const MmArgs& g, int64_t b, int64_t i0, i
 // Bound by the matrix cores where a CU has many pieces (2048 x 8192, two parts: Gram
 // product 107 us, step 194 us, 1060 TFLOP/s of f16, a product of the small side 35 us);
 // small ones by the launch, the first loads and the stores, 4 to 5 us, and the tiles'
-// bytes from L2, about 60 KB a microsecond and CU (12 of 512 x 512, one part: 7.3 us,
-// the step, whose three arrays are 31 MB in and out, 13.5).
+// bytes from L2, about 60 KB a microsecond and CU (12 of 512 x 512, one part: 7.5 us,
+// the step, whose three arrays are 46 MB in and out, 13.3).
 template <Prod P, int KIND, int T, bool MUON, bool SLICED, class Q>
 __global__ __launch_bounds__(Q::kThreads, 2) void k_mm(MmArgs g) {
   typedef typename Q::template Tile<P> Tile;
@@ -484,6 +498,13 @@ __global__ __launch_bounds__(Q::kThreads, 2) void k_mm(MmArgs g) {
   mm_tile<KIND>(g, tile, &im, &in);
   const int32_t p0 = slice * g.per, pieces = SLICED ? min(g.per, g.pieces - p0) : g.pieces;
   const int64_t i0 = (int64_t)im * TM, j0 = (int64_t)in * TN, at = (int64_t)p0 * kPiece;
+  const int wave = threadIdx.x >> 6;
+  const int64_t iw = i0 + (wave / WN) * (TM / WM), jw = j0 + (wave % WN) * (TN / WN);
+  // of a small tile, what joins its sums is under way from the start (12 updates of
+  // 512 x 512 BF16 139.6 us without, 134.6 so; 1024 x 1024 FP32 184 and 177)
+  constexpr bool EARLY = !SLICED && Tile::FN == 2;
+  Old<Tile::FM> old;
+  if (EARLY && threadIdx.x < Tile::kThreads) fetch_old<P, KIND, MUON>(g, b, iw, jw, old);
   mv4f acc[Tile::FM][Tile::FN];
   Tile::run(g.a + b * g.sa + i0 * g.lda + at, g.lda, (int32_t)(g.m - i0), g.b + b * g.sb + j0 * g.ldb + at, g.ldb,
             (int32_t)(g.n - j0), pieces, acc);
@@ -497,7 +518,6 @@ __global__ __launch_bounds__(Q::kThreads, 2) void k_mm(MmArgs g) {
       for (int i = 0; i < Tile::FM; ++i) d[(j * Tile::FM + i) * Tile::kThreads] = acc[i][j];
     return;
   }
-  const int wave = threadIdx.x >> 6;
   uint16_t* lds = (uint16_t*)(Tile::template stage<0>() + wave * (Tile::kStage / (WM * WN)));
   static_assert(32 * (16 * Tile::FM + 8) * 2 <= Tile::kStage / (WM * WN), "a wave's part of a stage");
 #pragma unroll
@@ -507,8 +527,8 @@ __global__ __launch_bounds__(Q::kThreads, 2) void k_mm(MmArgs g) {
     for (int i = 0; i < Tile::FM; ++i)
 #pragma unroll
       for (int r = 0; r < 8; ++r) s[i][r] = acc[i][j + (r >> 2)][r & 3];
-    finish<P, KIND, T, MUON, Tile::FM>(g, b, i0 + (wave / WN) * (TM / WM), j0 + (wave % WN) * (TN / WN) + j * 16,
-                                       KIND == STEP || im != in, lds, s);
+    if (!EARLY) fetch_old<P, KIND, MUON>(g, b, iw, jw + j * 16, old);
+    finish<P, KIND, T, MUON, Tile::FM>(g, b, iw, jw + j * 16, KIND == STEP || im != in, lds, s, old);
   }
 }
 
@@ -548,8 +568,9 @@ __global__ __launch_bounds__(64 * Q::WM * Q::WN) void k_sum(MmArgs g) {
       }
   }
   const int wave = threadIdx.x >> 6;
+  Old<FM> none;
   finish<P, GRAM, 0, false, FM>(g, b, (int64_t)im * TM + (wave / WN) * (TM / WM),
-                                (int64_t)in * TN + (wave % WN) * (TN / WN) + j * 16, im != in, lds[wave], s);
+                                (int64_t)in * TN + (wave % WN) * (TN / WN) + j * 16, im != in, lds[wave], s, none);
 }
 
 template <Prod P, int KIND, int T, bool MUON>
