@@ -27,8 +27,8 @@ constexpr int kBlock = 256;
 // Rows by groups of G threads (64: four rows a workgroup, 256: one), NV vectors of
 // 8 elements a thread in registers; NV = 0: a row of any length, read twice.
 // colw (nullable): every element is first multiplied by its column's weight.
-// 8192 x 2048: BF16 13.4 us (3.8 TB/s), FP32 16.7 us (5.0 TB/s); 16384 x 8192 BF16 95 us
-// (4.2 TB/s).
+// 8192 x 2048: BF16 12.5 us (4.0 TB/s), FP32 14.7 us (5.7 TB/s, a part of it from the
+// memory-side cache); 16384 x 8192 BF16 72.6 to 83 us (5.5 to 4.9 TB/s).
 template <int T, int MODE, int G, int NV, bool WEIGHTED>
 __global__ __launch_bounds__(kBlock) void k_rows_i8(const typename Elem<T>::type* __restrict__ src, int64_t rows,
                                                     int64_t cols, int64_t ld, const float* __restrict__ colw,
@@ -134,7 +134,7 @@ __device__ __forceinline__ void store_tile_t(const TileT<COLS>& tile, int8_t* qt
 }
 
 // INT8 [rows][ld] -> [cols][ldt], zeros for the rows past the last.  128 x 128 tiles.
-// 8192 x 2048: 7.1 us (4.7 TB/s).
+// 8192 x 2048: 6.9 us (4.9 TB/s).
 __global__ __launch_bounds__(kBlock) void k_transpose_i8(const int8_t* __restrict__ q, int64_t rows, int64_t cols,
                                                          int64_t ld, int8_t* __restrict__ qt, int64_t ldt,
                                                          uint32_t ctiles) {
@@ -158,8 +158,8 @@ __global__ __launch_bounds__(kBlock) void k_transpose_i8(const int8_t* __restric
 }
 
 // Column maxima of |x[r][c] roww[r]| and column sums of x over slices of the rows:
-// workgroups of 64 columns by one slice, 32 rows at a time.  8192 x 2048 BF16: 9.3 us
-// (3.6 TB/s; four rows a thread in flight, with eight 9.7).
+// workgroups of 64 columns by one slice, 32 rows at a time.  8192 x 2048 BF16: 8.9 us
+// (3.8 TB/s; four rows a thread in flight).
 template <int T>
 __global__ __launch_bounds__(kBlock) void k_col_max(const typename Elem<T>::type* __restrict__ src, int64_t rows,
                                                     int64_t cols, const float* __restrict__ roww, int64_t slice,
@@ -220,7 +220,7 @@ __global__ __launch_bounds__(kBlock) void k_col_max(const typename Elem<T>::type
 // 64 columns, a thread 4 x 8 of them.  The columns' scales come from the slices'
 // maxima, at most kMostParts of them, in every tile; the first row of tiles writes them
 // and the columns' sums (a launch of its own for that took 3.4 to 4.6 us).  8192 x
-// 2048 BF16: 17.4 us (2.9 TB/s: reads of 128 bytes a row, and the rounding).
+// 2048 BF16: 10.6 us (4.7 TB/s).
 constexpr int kMostParts = 32;
 template <int T, int MODE>
 __global__ __launch_bounds__(kBlock) void k_col_i8_t(const typename Elem<T>::type* __restrict__ src, int64_t rows,
