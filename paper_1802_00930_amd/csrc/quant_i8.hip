@@ -321,8 +321,8 @@ dfp_status launch_rows_i8(int32_t type, int32_t rounding, uint64_t seed, uint32_
       auto by_len = [&](auto weighted) -> dfp_status {
         typedef std::integral_constant<int, 64> Wave;
         typedef std::integral_constant<int, 256> Group;
-        // a wave a row up to 2048 (8192 x 2048 BF16 9.8 us; by workgroups 15.6), or 16 waves for a
-        // few long rows, a workgroup up to 16384
+        // a wave a row up to 2048 (8192 x 2048 BF16 14.2 us; by workgroups 14.7); by workgroups for
+        // few such rows (their waves share the loads) and up to 16384
         if (nvec <= 64) return go(Wave(), std::integral_constant<int, 1>(), weighted);
         if (nvec <= 128) return go(Wave(), std::integral_constant<int, 2>(), weighted);
         if (nvec <= 256 && rows > 512) return go(Wave(), std::integral_constant<int, 4>(), weighted);
