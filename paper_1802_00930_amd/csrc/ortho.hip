@@ -678,23 +678,26 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
     // Q = B = b A + c A A, and what further iterations make of it; X = q X + Q X in the end
     uint8_t* q = bb;
     float uq = 1.f;
-    double qa = 1., grown = 1.;
+    double qa = 1., grown = 1., top = 1.;
     for (int32_t k = 0;; ++k, ++s) {
       const float ca = d.coef[s][0], cb = d.coef[s][1], cc = d.coef[s][2];
       const float ub = unit_for(std::fabs((double)cb) * 2. + std::fabs((double)cc) * 4.);
+      const double most = most_of(ca, cb, cc);
       uint8_t* to = k == 0 && MUON && p.grouped ? qq[0] : bb;
       g.ca = ca;
       if ((rc = small(aa, aa, to, cc * kInvA * kInvA, aa, cb * kInvA, ub)) != DFP_OK) return rc;
       if (k == 0) {
         q = to, uq = ub;
       } else {
-        const float un = unit_for(2. * std::fabs(qa * ca));
+        // |P_2 P_1|: to the first X of a singular value above 1 the product of the steps'
+        // largest on [0, 1], and from there 4, since no X ends above it
+        const float un = unit_for(std::max(std::sqrt(grown) * most, 4. * top) + std::fabs(qa * ca));
         if ((rc = small(bb, q, qq[k & 1], 1.f / (ub * uq), q, ca / uq, un, bb, (float)qa / ub)) != DFP_OK) return rc;
         q = qq[k & 1], uq = un;
       }
       qa *= ca;
-      const double most = most_of(ca, cb, cc);
       grown *= most * most;
+      top = std::max(top, std::sqrt(grown));
       if (!MUON || !p.grouped || s + 1 >= d.steps || grown > 150.) break;
       // A = P A P
       const float ua = (float)(1 << kUnitA);

@@ -1,0 +1,73 @@
+"""Weight steps by orthogonalised momentum whose polynomials differ from step to step: ones that take iterations
+together on the small side, and what they hold in f16 on the way.
+
+Tolerance: an update is within twice of what the same iterations in FP32 give, and iterations taken together within
+three times of that (dfp.h): six times the distance of FP32 products from 64 bits, both measured here, or of 2^-22,
+what an operand of two f16 numbers is off by, where FP32 comes nearer than that."""
+import pytest
+import torch
+
+from gpu_helpers import DEV, note
+from paper_1802_00930_amd import dfp
+
+pytestmark = pytest.mark.gpu
+
+
+def iterate(u, steps, dtype, eps=1e-7):
+    """(the orthogonalised u, the largest singular value of X before and after any step)."""
+    x = u.double()
+    x = x.t().contiguous() if u.shape[0] > u.shape[1] else x
+    x = (x / (torch.linalg.vector_norm(x) + eps)).to(dtype)
+    largest = 0.0
+    for a, b, c in steps:
+        g = torch.mm(x, x.t().contiguous())
+        x = a * x + torch.mm(b * g + c * torch.mm(g, g), x)
+        if dtype is torch.float64:
+            largest = max(largest, float(torch.linalg.eigvalsh(torch.mm(x, x.t().contiguous()).cpu())[-1]) ** 0.5)
+    return (x.t() if u.shape[0] > u.shape[1] else x).double(), largest
+
+
+def update(dw, steps):
+    """O(dw): w = 0 and lr scale = 1 leave -O(u), v = 0 and mu = 0 make u = dw."""
+    b, r, c = dw.shape
+    d = dfp.make_ortho_desc(b, r, c, dw.dtype, steps=len(steps), coef=steps)
+    raw = torch.zeros(b * r * c + 64, device=DEV)
+    raw[b * r * c:] = 7
+    w, v = raw[:b * r * c].view(b, r, c), torch.zeros(b, r, c, device=DEV)
+    ws = torch.full((dfp.ortho_workspace_bytes(d),), 0xff, dtype=torch.uint8, device=DEV)
+    dfp.dfp_muon_quantize(d, 1.0, 0.0, 0.0, 1.0, w, v, dw, workspace=ws)
+    assert torch.equal(v, dw.float()) and bool((raw[b * r * c:] == 7).all())
+    return -w
+
+
+def normal(seed, *shape):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return torch.randn(*shape, generator=g, device=DEV)
+
+
+def assert_near(got, u, steps, times=6.0):
+    want, largest = iterate(u, steps, torch.float64)
+    plain, _ = iterate(u, steps, torch.float32)
+    norm = torch.linalg.vector_norm(want)
+    off, fp32 = (float(torch.linalg.vector_norm(y - want) / norm) for y in (got.double(), plain))
+    print("off %.2e, FP32 %.2e, largest singular value %.2f" % (off, fp32, largest), flush=True)
+    assert largest <= 4  # what the call is documented for
+    assert off <= times * max(fp32, 2.0 ** -22), (off, fp32)  # (not so for NaN)
+    return largest
+
+
+# small at 0 and large away from it, alone or after one another: P_2 P_1 - q is far above q
+AWAY_FROM_ZERO = {"zero": [(5.0, -20.0, 16.0), (0.0, 20.0, -20.0)],
+                  "half": [(5.0, -20.0, 16.0), (0.5, 18.0, -18.0)],
+                  "twice": [(5.0, -20.0, 16.0), (0.0, 20.0, -20.0), (0.25, 0.0, 0.0)] * 2}
+
+
+@pytest.mark.parametrize("name", list(AWAY_FROM_ZERO))
+@pytest.mark.parametrize("b,r,c", [(1, 51, 8000), (1, 8000, 51), (3, 40, 3000), (1, 100, 5000)])
+def test_polynomials_that_are_large_away_from_zero(b, r, c, name):
+    note("weight step %dx%dx%d %s" % (b, r, c, name))
+    dw = 1e-3 * normal(r + c, b, r, c)
+    got = update(dw, AWAY_FROM_ZERO[name])
+    for i in range(b):
+        assert_near(got[i], dw[i], AWAY_FROM_ZERO[name])
