@@ -525,8 +525,8 @@ size_t dfp_linear_i8_workspace_bytes(const dfp_linear_desc* d);
  * sum of two f16 numbers and every product the sum of three: 1e-6 to 2e-5, within twice
  * of what FP32 products give; dfp_muon_quantize on matrices much longer one way up to
  * three times that (it takes iterations together).  The units suit singular values up
- * to 4 at every step (a, b, c that map [0, 1] further out overflow f16 and give Inf or
- * NaN) and norms not below eps by more than a factor of 2^10 (smaller ones lose bits).
+ * to 4 before and after every step (a, b, c that map [0, 1] further out overflow f16 and
+ * give Inf or NaN) and norms not below eps by more than a factor of 2^10 (smaller ones lose bits).
  * A zero matrix gives zeros; one with NaN or Inf gives NaN throughout. */
 #define DFP_ORTHO_MAX_STEPS 16
 typedef struct dfp_ortho_desc {

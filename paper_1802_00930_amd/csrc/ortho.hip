@@ -25,8 +25,8 @@
 // computed from X again: 2 to 3 times the error of single iterations, of an update that
 // enters FP32 weights times lr.
 //
-// Units: X in 2^-12, A in 2^-10, B in 2^-sb so that |b A + c A A| <= 32768 in it for
-// singular values up to sqrt(2).
+// Units: X in 2^-12, A in 2^-10, which hold singular values up to 4 twice over; B and Q in
+// one that holds what such values, before and after the step, can make of them (unit_b, run).
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -617,6 +617,13 @@ float unit_for(double most) {
   return (float)(1 << s);
 }
 
+// Unit of B = b A + c A A.  Up to A = 2: by its terms.  From there to 16: by its terms, or,
+// since |a + B| sqrt(A) <= 4 after the step, |B| <= |a| + 4 / sqrt(2).
+float unit_b(double a, double b, double c) {
+  a = std::fabs(a), b = std::fabs(b), c = std::fabs(c);
+  return unit_for(std::max(2. * b + 4. * c, std::min(16. * b + 256. * c, a + 2.83)));
+}
+
 template <int T, bool MUON, Prod P>
 dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* w, float alpha, float keep, void* ws,
                hipStream_t st) {
@@ -681,7 +688,7 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
     double qa = 1., grown = 1., top = 1.;
     for (int32_t k = 0;; ++k, ++s) {
       const float ca = d.coef[s][0], cb = d.coef[s][1], cc = d.coef[s][2];
-      const float ub = unit_for(std::fabs((double)cb) * 2. + std::fabs((double)cc) * 4.);
+      const float ub = unit_b(ca, cb, cc);
       const double most = most_of(ca, cb, cc);
       uint8_t* to = k == 0 && MUON && p.grouped ? qq[0] : bb;
       g.ca = ca;

@@ -71,3 +71,47 @@ def test_polynomials_that_are_large_away_from_zero(b, r, c, name):
     got = update(dw, AWAY_FROM_ZERO[name])
     for i in range(b):
         assert_near(got[i], dw[i], AWAY_FROM_ZERO[name])
+
+
+# A strong direction reaches 3.9, a singular value that the second step nearly takes to 0: a is large, and B's
+# entries are as large there, far above what b and c give up to 2.
+STEEP = [(3.9, 0.0, 0.0), (64.0, 0.0, -0.2766)]
+
+
+def one_strong_direction(r, c):
+    """Its left side on two rows, so that B's entries there are on and off the diagonal; a hundredth of it beside it."""
+    left = torch.zeros(r, 1, device=DEV)
+    left[0] = left[5] = 0.5 ** 0.5
+    right, rest = normal(r, 1, c), normal(r + 1, r, c)
+    right = right / torch.linalg.vector_norm(right)
+    return 1e-3 * (left * right + 0.01 * rest / torch.linalg.matrix_norm(rest.cpu(), 2).to(DEV))
+
+
+@pytest.mark.parametrize("steps", [STEEP, STEEP + [(0.3, 0.1, -0.01)]])
+@pytest.mark.parametrize("r,c", [(24, 40), (24, 2000), (2000, 24), (70, 90)])
+def test_weight_step_near_the_largest_singular_value(r, c, steps):
+    note("weight step %dx%d at 3.9" % (r, c))
+    dw = one_strong_direction(min(r, c), max(r, c))
+    dw = (dw.t().contiguous() if r > c else dw)[None]
+    assert assert_near(update(dw, steps)[0], dw[0], steps) > 3.8
+
+
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("r,c", [(24, 40), (40, 24), (70, 90)])
+def test_update_near_the_largest_singular_value(r, c, t):
+    """BF16: of B, whose entries sum to |B| <= 64 in squares, of A <= 16, times dB/dA <= 2 16 0.2766, and of X <= 4 a
+    rounding is 2^-12: 2^-12 (64 4 + 16 8.9 4 + 64 4) = 0.27 in all; then 2^-9 of the other step and the result's
+    2^-8."""
+    note("update %dx%d at 3.9 %s" % (r, c, t))
+    x = one_strong_direction(min(r, c), max(r, c))
+    x = (x.t().contiguous() if r > c else x).to(t)[None]
+    d = dfp.make_ortho_desc(1, r, c, t, steps=2, coef=STEEP)
+    out = torch.empty_like(x)
+    dfp.dfp_orthogonalize(d, x, out, workspace=dfp.alloc_ortho_workspace(d))
+    if t is torch.float32:
+        assert_near(out[0], x[0], STEEP)
+        return
+    want, largest = iterate(x[0], STEEP, torch.float64)
+    off, norm = torch.linalg.vector_norm(out[0].double() - want), torch.linalg.vector_norm(want)
+    print("off %.3f of %.1f, largest singular value %.2f" % (off, norm, largest), flush=True)
+    assert 3.8 < largest <= 4 and off <= 0.27 + (2.0 ** -9 + 2.0 ** -8) * norm
