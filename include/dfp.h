@@ -519,14 +519,20 @@ size_t dfp_linear_i8_workspace_bytes(const dfp_linear_desc* d);
  * which applies x -> a x + b x^3 + c x^5 to the singular values.
  * Precision: X is held as the sum of two f16 numbers (2^-24 of a value), every sum
  * in FP32.  BF16 results: the products take X, A and B rounded to one f16 number (X
- * in units of 2^-12, A of 2^-10, B's diagonal apart in FP32): 0.4e-3 to 0.9e-3 of the
- * result's norm for matrices of some size, at most 2^-9, half of BF16's half step, for a
- * few elements too.  FP32 and F16 results and dfp_muon_quantize: every operand is the
- * sum of two f16 numbers and every product the sum of three: 1e-6 to 2e-5, within twice
- * of what FP32 products give; dfp_muon_quantize on matrices much longer one way up to
- * three times that (it takes iterations together).  The units suit singular values up
- * to 4 before and after every step (a, b, c that map [0, 1] further out overflow f16 and
- * give Inf or NaN) and norms not below eps by more than a factor of 2^10 (smaller ones lose bits).
+ * in units of 2^-12, A of 2^-10, B's diagonal apart in FP32), which with the usual
+ * coefficients (3.4445, -4.775, 2.0315) adds 0.1e-3 to 1.7e-3 of the result's norm,
+ * less than half of BF16's half step, to its rounding; x and out of type F32 are
+ * the call without that.  FP32 results, F16 results up to their own rounding and
+ * dfp_muon_quantize: every operand is the sum of two f16 numbers and every product
+ * the sum of three, which is as near as FP32 products come, within 2.5 times:
+ * 0.5e-6 to 1e-4 with those coefficients, the more the weaker most directions are
+ * beside the strongest.  dfp_muon_quantize takes iterations on matrices much longer
+ * one way together, where an error of A, 2^-22, may grow: up to 4e-5 with those
+ * coefficients also where FP32 products give 1e-6; steeper ones, which could take
+ * it past 4e-4, are not taken together.  Large coefficients that cancel lose more, as in FP32.
+ * The units suit singular values up to 4 before and after every step (a, b, c that
+ * map [0, 1] further out overflow f16 and give Inf or NaN) and norms not below eps
+ * by more than a factor of 2^10 (smaller ones lose bits).
  * A zero matrix gives zeros; one with NaN or Inf gives NaN throughout. */
 #define DFP_ORTHO_MAX_STEPS 16
 typedef struct dfp_ortho_desc {

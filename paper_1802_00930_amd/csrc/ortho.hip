@@ -21,9 +21,11 @@
 // X = P_2 P_1 X = q X + Q X with q = a_2 a_1, Q = a_2 B_1 + a_1 B_2 + B_2 B_1.  That replaces a
 // Gram product and a step by three products of the small side.  An error of A grows by
 // the square of P's norm an iteration, m = a^2 where a is the largest that a + b s + c s^2
-// gets on [0, 1], so no more than m m' <= 150 (two such for a = 3.44) are taken before A is
-// computed from X again: 2 to 3 times the error of single iterations, of an update that
-// enters FP32 weights times lr.
+// gets on [0, 1], and enters the next polynomial by its slope, |b| + 2 |c| at most.  So A is
+// computed from X again once m m' is above 150 (two iterations of a = 3.44) or, times the next
+// slope, above 1600 (1244 there): 2^-22 of A become 4e-4 of the update at worst, and measured
+// up to 4e-5 with those coefficients, where single iterations and FP32 products may end at
+// 1e-6, of an update that enters FP32 weights times lr.
 //
 // Units: X in 2^-12, A in 2^-10, which hold singular values up to 4 twice over; B and Q in
 // one that holds what such values, before and after the step, can make of them (unit_b, run).
@@ -706,6 +708,7 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
       grown *= most * most;
       top = std::max(top, std::sqrt(grown));
       if (!MUON || !p.grouped || s + 1 >= d.steps || grown > 150.) break;
+      if (grown * (std::fabs(d.coef[s + 1][1]) + 2. * std::fabs(d.coef[s + 1][2])) > 1600.) break;
       // A = P A P
       const float ua = (float)(1 << kUnitA);
       if ((rc = small(to, aa, pa, kInvA / ub, aa, ca * kInvA, ua)) != DFP_OK) return rc;
