@@ -2,10 +2,9 @@
 #pragma once
 
 #include "dfp_internal.h"
+#include "mm_plan.h"
 
 namespace dfp {
-
-inline int64_t i8_ld(int64_t cols) { return (cols + 127) / 128 * 128; }
 
 // Rows of src (times colw of the column, nullable) to q [rows][i8_ld(cols)] and scale [rows].
 dfp_status launch_rows_i8(int32_t type, int32_t rounding, uint64_t seed, uint32_t role, const void* src, int64_t rows,
@@ -22,13 +21,8 @@ dfp_status launch_cols_i8_t(int32_t type, int32_t rounding, uint64_t seed, uint3
                             int64_t rows, int64_t cols, const float* roww, int8_t* qt, float* scale, float* sums,
                             void* ws, hipStream_t st);
 
-// out [m][n] (type) = (sum over k of a b) sa[m] sb[n] + bias[n]; sb, bias nullable.  ws: plan_gemm_i8(...).bytes.
-struct I8Plan {
-  int32_t kind;         // of tile (mma_tile.h); -1: the kernel for few rows
-  int32_t slices, per;  // of the reduction, pieces in each
-  int64_t bytes;        // the slices' sums
-};
-I8Plan plan_gemm_i8(int64_t m, int64_t n, int64_t k);
+// out [m][n] (type) = (sum over k of a b) sa[m] sb[n] + bias[n]; sb, bias nullable.  ws: plan_gemm_i8(...).bytes
+// (mm_plan.h).
 dfp_status launch_gemm_i8(int32_t m, int32_t n, int32_t k, const int8_t* a, const float* sa, const int8_t* b,
                           const float* sb, const float* bias, int32_t type, void* out, void* ws, hipStream_t st);
 // The forward call for a few tokens in one launch, where fits_token_i8.

@@ -286,46 +286,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 4) void k_token(I8Args g, const typ
   }
 }
 
-// The kernel of a product by an estimate of its time (us).
-//   k_few    a CU takes 0.15, 0.21 or 0.35 for a piece of 16 columns by up to 16, 32
-//            or 64 rows (4096 x 4096, 8192 x 2048 and 8192 x 8192 weights).
-//   k_tiles  tile_us; with weights that come from memory, as they do for few rows, a
-//            quarter more.  Slices mean that their sums are written and read (4 TB/s)
-//            and a second kernel (4).
-// At 64 rows: 4096 x 4096 k_few 13.8, tiles 12.0; 8192 x 2048 13.4 and 8.2; 8192 x
-// 8192 44.7 and 22.1; 1024 x 1024 5.0 and 5.1.  At 24: 9.7 and 10.0; 8.6 and 7.3; 25.4 and
-// 20.4; 3.5 and 4.7.  At 16, where k_few runs always: 7.9 and 9.7; 7.0 and 7.0; 19.4 and
-// 20.3; 3.2 and 4.5.
-constexpr int32_t kFewRows = 64;
-constexpr int64_t kMostPartBytes = 64 << 20;
-
 }  // namespace
-
-I8Plan plan_gemm_i8(int64_t m, int64_t n, int64_t k) {
-  I8Plan best{-1, 1, 0, 0};
-  const int64_t pieces = i8_ld(k) / kPiece;
-  double least = 1e30;
-  if (m <= kFewRows) {
-    least = 2. + ((n + 15) / 16 + 255) / 256 * pieces * (m <= 16 ? 0.15 : m <= 32 ? 0.21 : 0.35);
-    if (m <= 16) return best;
-  }
-  for (int t = 0; t < kTileKindCount; ++t) {
-    const TileKind& kind = kTileKinds[t];
-    const int64_t tiles = ((m + kind.tm - 1) / kind.tm) * ((n + kind.tn - 1) / kind.tn);
-    for (int64_t slices = 1; slices <= 16 && slices <= pieces; slices *= 2) {
-      const int64_t per = (pieces + slices - 1) / slices, used = (pieces + per - 1) / per;
-      const int64_t bytes = used > 1 ? used * m * n * 4 : 0;
-      if (bytes > kMostPartBytes) break;
-      double us = tile_us(kind, false, tiles * used, per, m <= kFewRows ? 1.25 : 1.);
-      if (used > 1) us += 4. + 2. * bytes / 4e6;
-      if (us < least) {
-        least = us;
-        best = {t, (int32_t)used, (int32_t)per, bytes};
-      }
-    }
-  }
-  return best;
-}
 
 bool fits_token_i8(int64_t m, int64_t k) {
   return m <= kTokenRows && i8_ld(k) <= (int64_t)64 * 8 * kTokenVecs << token_shift(m);

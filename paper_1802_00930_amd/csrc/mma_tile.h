@@ -15,6 +15,7 @@
 #include <utility>
 
 #include "dfp_internal.h"
+#include "mm_plan.h"
 
 namespace dfp {
 
@@ -42,8 +43,6 @@ __device__ __forceinline__ typename MmaTypes<P>::acc_t mma16(const mv4i& rows, c
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(mv8h, rows), __builtin_bit_cast(mv8h, cols), c, 0,
                                                   0, 0);
 }
-
-constexpr int kPiece = 128;  // bytes of a row per step of the loop
 
 typedef __attribute__((address_space(3))) void* mma_lds_t;
 
@@ -220,12 +219,7 @@ struct MmaTile {
   }
 };
 
-// The tiles in use and an estimate of a product's time (us), from products of 64 to 1024
-// tiles (`tiles` / 256 rounded up: the most a CU has) at reductions of 32 and 96 pieces:
-//   start + (rounds - 1) start_round + pieces (piece, from 128 to 256 tiles rising to
-//   piece_full, + (rounds - 1) piece_round)
-// for I8 and F16, and for F16X2.  Outputs of a tile per time rise with its side, but so
-// does what starts and ends it, and 256 CUs are filled in steps.
+// The tiles in use, kTileKinds of mm_plan.h.
 template <int TM_, int TN_, int WM_, int WN_, int S_, int KG_ = 1>
 struct TileShape {
   static constexpr int TM = TM_, TN = TN_, WM = WM_, WN = WN_, S = S_, KG = KG_;
@@ -233,25 +227,6 @@ struct TileShape {
   template <Prod P>
   using Tile = MmaTile<P, TM, TN, WM, WN, S, KG>;
 };
-struct TileCost {
-  double start, start_round, piece, piece_full, piece_round;
-};
-struct TileKind {
-  int32_t tm, tn;
-  TileCost cost[2];
-};
-constexpr TileKind kTileKinds[] = {
-    {256, 256, {{14.0, 12.5, 1.23, 1.61, 1.60}, {14.5, 13.0, 1.55, 2.14, 2.12}}},
-    {192, 192, {{8.6, 7.0, 0.77, 0.96, 0.95}, {8.5, 7.5, 0.96, 1.29, 1.25}}},
-    {192, 128, {{5.5, 5.5, 0.71, 0.76, 0.58}, {6.8, 5.0, 0.70, 0.92, 0.80}}},
-    {128, 128, {{5.0, 4.0, 0.63, 0.63, 0.41}, {6.0, 4.0, 0.61, 0.67, 0.56}}},
-    {96, 96, {{4.0, 2.3, 0.35, 0.37, 0.36}, {4.5, 2.3, 0.39, 0.43, 0.44}}},
-    {64, 64, {{1.0, 1.8, 0.28, 0.30, 0.16}, {1.7, 1.4, 0.29, 0.30, 0.17}}},
-    {64, 64, {{2.3, 2.2, 0.20, 0.21, 0.20}, {3.1, 2.5, 0.20, 0.22, 0.21}}},     // two groups each
-    {128, 128, {{6.5, 5.0, 0.47, 0.53, 0.51}, {7.5, 6.5, 0.49, 0.59, 0.60}}},
-    {96, 96, {{5.5, 4.0, 0.30, 0.29, 0.31}, {6.5, 4.3, 0.30, 0.33, 0.36}}},
-};
-constexpr int kTileKindCount = 9;
 template <class F>
 dfp_status with_tile(int32_t kind, F f) {
   switch (kind) {
@@ -265,14 +240,6 @@ dfp_status with_tile(int32_t kind, F f) {
     case 7: return f(TileShape<128, 128, 2, 2, 2, 2>());
     default: return f(TileShape<96, 96, 2, 3, 3, 2>());
   }
-}
-// slow: what the reduction takes more when operands come from memory.
-inline double tile_us(const TileKind& k, bool split, int64_t tiles, int64_t pieces, double slow = 1.) {
-  const TileCost& c = k.cost[split];
-  const double more = (double)((tiles + 255) / 256 - 1);
-  const double full = tiles >= 256 ? 1. : tiles <= 128 ? 0. : (double)(tiles - 128) / 128.;
-  return c.start + more * c.start_round +
-         (double)pieces * slow * (c.piece + full * (c.piece_full - c.piece) + more * c.piece_round);
 }
 
 // Consecutive workgroups go round the 8 XCDs, each with an L2 of its own: this turns

@@ -48,55 +48,13 @@ constexpr int kBlock = 256;
 constexpr int kUnitX = 12, kUnitA = 10;
 constexpr int kNormParts = 1024;  // most partial sums of a matrix
 
-// A product's tiles and slices by an estimate of its time: tile_us and 2 us a round for
-// 128 x 128 outputs (which are stored twice, after another pass through LDS); slices
-// mean that their sums are written and read (5 TB/s) and a second kernel (4 us).
-struct MmPlan {
-  int32_t kind, slices, per;
-  int64_t bytes;
-  double us;
-};
-constexpr int64_t kMostPartBytes = 128 << 20;
-
-// Tiles of the symmetric products: square, and of two parts not 96 x 96 by one group,
-// which two groups always beat (kTileKinds[4] and [8]).
-constexpr bool has_triangle(int kind, bool split) {
-  return kTileKinds[kind].tm == kTileKinds[kind].tn && !(split && kind == 4);
-}
-
-MmPlan plan_mm(int64_t m, int64_t n, int64_t pieces, int64_t batch, bool symmetric, bool sliceable, bool split) {
-  MmPlan best{};
-  double least = 1e30;
-  for (int t = 0; t < kTileKindCount; ++t) {
-    const TileKind& kind = kTileKinds[t];
-    if (symmetric && !has_triangle(t, split)) continue;
-    const int64_t tm = (m + kind.tm - 1) / kind.tm, tn = (n + kind.tn - 1) / kind.tn;
-    const int64_t tiles = (symmetric ? tm * (tm + 1) / 2 : tm * tn) * batch;
-    for (int64_t s = 1; s <= (sliceable ? 32 : 1) && s <= pieces; ++s) {
-      const int64_t per = (pieces + s - 1) / s, used = (pieces + per - 1) / per;
-      if (used != s) continue;
-      const int64_t bytes = s > 1 ? s * tiles * kind.tm * kind.tn * 4 : 0;
-      if (bytes > kMostPartBytes) break;
-      double us = tile_us(kind, split, tiles * s, per) +
-                  2. * ((tiles * s + 255) / 256) * kind.tm * kind.tn / 16384.;
-      if (s > 1) us += 4. + 2. * bytes / 5e6;
-      if (us < least) {
-        least = us;
-        best = {t, (int32_t)s, (int32_t)per, bytes, us};
-      }
-    }
-  }
-  return best;
-}
-
 struct Plan {
   bool tall;             // rows > cols
   int64_t R, C, Rp, Cp;  // the matrix, padded
   int64_t r, rp;         // the smaller side, padded
   int64_t e;             // bytes of an operand element
   int64_t xlo, gram, step0, step1, aa, bb, pa, qq0, qq1, diag, norm, slices, bytes;  // offsets, total
-  MmPlan mgram, mpoly, mstep;
-  bool grouped;          // weight steps: iterations on the small side (3 us a launch)
+  OrthoPlan mm;
 };
 
 Plan make_plan(const dfp_ortho_desc& d, bool split) {
@@ -116,24 +74,19 @@ Plan make_plan(const dfp_ortho_desc& d, bool split) {
     return o;
   };
   const int64_t n = p.Rp * p.Cp * d.batch, s = p.rp * p.rp * d.batch;
-  const int64_t per_piece = split ? 32 : 64;
-  // (only the Gram product has reductions longer than its sides)
-  p.mgram = plan_mm(p.rp, p.rp, (p.tall ? p.Rp : p.Cp) / per_piece, d.batch, true, true, split);
-  p.mpoly = plan_mm(p.rp, p.rp, p.rp / per_piece, d.batch, true, false, split);
-  p.mstep = plan_mm(p.Rp, p.Cp, p.rp / per_piece, d.batch, false, false, split);
+  p.mm = plan_ortho(d.batch, p.R, p.C, split);
   p.xlo = take(split ? 0 : n * 2);
   p.gram = take(n * p.e);
   p.step0 = take(n * p.e);
   p.step1 = take(n * p.e);
   p.aa = take(s * p.e);
   p.bb = take(s * p.e);
-  p.grouped = split && p.mgram.us + p.mstep.us > 3. * p.mpoly.us + 3.;
-  p.pa = take(p.grouped ? s * p.e : 0);
-  p.qq0 = take(p.grouped ? s * p.e : 0);
-  p.qq1 = take(p.grouped ? s * p.e : 0);
+  p.pa = take(p.mm.grouped ? s * p.e : 0);
+  p.qq0 = take(p.mm.grouped ? s * p.e : 0);
+  p.qq1 = take(p.mm.grouped ? s * p.e : 0);
   p.diag = take(split ? 0 : p.rp * d.batch * 4);
   p.norm = take((int64_t)kNormParts * d.batch * 8);
-  p.slices = take(p.mgram.bytes);
+  p.slices = take(p.mm.gram.bytes);
   p.bytes = at;
   return p;
 }
@@ -664,7 +617,7 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
     g.old2 = y, g.cold2 = c2;
     g.uout = uout;
     g.rowop = g.colop = to;
-    return launch_mm<P, POLY, 0, false>(K_ORTHO_POLY, p.mpoly, d.batch, g, st);
+    return launch_mm<P, POLY, 0, false>(K_ORTHO_POLY, p.mm.poly, d.batch, g, st);
   };
   dfp_status rc;
   for (int32_t s = 0, turn = 0; s < d.steps; ++turn) {
@@ -683,7 +636,7 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
     g.rowop = g.colop = aa;
     g.ldr = g.ldc = p.rp * p.e;
     g.sr = g.sc = ss;
-    if ((rc = launch_mm<P, GRAM, 0, false>(K_ORTHO_GRAM, p.mgram, d.batch, g, st)) != DFP_OK) return rc;
+    if ((rc = launch_mm<P, GRAM, 0, false>(K_ORTHO_GRAM, p.mm.gram, d.batch, g, st)) != DFP_OK) return rc;
     // Q = B = b A + c A A, and what further iterations make of it; X = q X + Q X in the end
     uint8_t* q = bb;
     float uq = 1.f;
@@ -692,7 +645,7 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
       const float ca = d.coef[s][0], cb = d.coef[s][1], cc = d.coef[s][2];
       const float ub = unit_b(ca, cb, cc);
       const double most = most_of(ca, cb, cc);
-      uint8_t* to = k == 0 && MUON && p.grouped ? qq[0] : bb;
+      uint8_t* to = k == 0 && MUON && p.mm.grouped ? qq[0] : bb;
       g.ca = ca;
       if ((rc = small(aa, aa, to, cc * kInvA * kInvA, aa, cb * kInvA, ub)) != DFP_OK) return rc;
       if (k == 0) {
@@ -707,7 +660,7 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
       qa *= ca;
       grown *= most * most;
       top = std::max(top, std::sqrt(grown));
-      if (!MUON || !p.grouped || s + 1 >= d.steps || grown > 150.) break;
+      if (!MUON || !p.mm.grouped || s + 1 >= d.steps || grown > 150.) break;
       if (grown * (std::fabs(d.coef[s + 1][1]) + 2. * std::fabs(d.coef[s + 1][2])) > 1600.) break;
       // A = P A P
       const float ua = (float)(1 << kUnitA);
@@ -737,9 +690,9 @@ dfp_status run(const dfp_ortho_desc& d, const Source<T>& src, void* out, float* 
     g.w = w;
     g.alpha = alpha, g.keep = keep;
     if (s < d.steps)
-      rc = launch_mm<P, STEP, 0, false>(K_ORTHO_STEP, p.mstep, d.batch, g, st);
+      rc = launch_mm<P, STEP, 0, false>(K_ORTHO_STEP, p.mm.step, d.batch, g, st);
     else
-      rc = launch_mm<P, LAST, MUON ? DFP_F32 : T, MUON>(K_ORTHO_STEP, p.mstep, d.batch, g, st);
+      rc = launch_mm<P, LAST, MUON ? DFP_F32 : T, MUON>(K_ORTHO_STEP, p.mm.step, d.batch, g, st);
     if (rc != DFP_OK) return rc;
   }
   return DFP_OK;
