@@ -526,10 +526,11 @@ size_t dfp_linear_i8_workspace_bytes(const dfp_linear_desc* d);
  * dfp_muon_quantize: every operand is the sum of two f16 numbers and every product
  * the sum of three, which is as near as FP32 products come, within 2.5 times:
  * 0.5e-6 to 1e-4 with those coefficients, the more the weaker most directions are
- * beside the strongest.  dfp_muon_quantize takes iterations on matrices much longer
- * one way together, where an error of A, 2^-22, may grow: up to 4e-5 with those
- * coefficients also where FP32 products give 1e-6; steeper ones, which could take
- * it past 4e-4, are not taken together.  Large coefficients that cancel lose more, as in FP32.
+ * beside the strongest.  dfp_muon_quantize takes iterations together where that is
+ * estimated to be faster (matrices longer one way), in which an error of A, 2^-22, may
+ * grow: up to 4e-5 with those coefficients also where FP32 products give 1e-6; steeper
+ * ones, which could take it past 4e-4, are not taken together.  Large coefficients
+ * that cancel lose more, as in FP32.
  * The units suit singular values up to 4 before and after every step (a, b, c that
  * map [0, 1] further out overflow f16 and give Inf or NaN) and norms not below eps
  * by more than a factor of 2^10 (smaller ones lose bits).
