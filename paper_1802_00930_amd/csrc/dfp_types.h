@@ -26,13 +26,10 @@ struct Elem<DFP_F16> {
   static __device__ __forceinline__ uint16_t down(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
 };
 
-inline int64_t type_bytes(int32_t type) { return type == DFP_F32 ? 4 : 2; }
-
 // N elements as they lie in memory, from p on (aligned to an element only; the vector
 // loads of gfx950 take that).  Loaded first and turned into numbers behind all
 // loads of a loop: fetch_n is a branch, and what uses the elements in it waits for
-// them there (16384 x 8192 BF16 by rows 85.5 us, 72.6 so; 8192 x 2048
-// FP32 19.0 and 16.7).
+// them there (16384 x 8192 BF16 by rows 85.5 us, 72.6 so).
 template <int T, int N>
 struct __attribute__((packed, aligned(sizeof(typename Elem<T>::type)))) Raw {
   uint32_t w[N * sizeof(typename Elem<T>::type) / 4];

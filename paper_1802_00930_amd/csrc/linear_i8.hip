@@ -4,7 +4,6 @@
 //   k_few    few rows (one token, a decoding batch): bound by the weights' bytes
 //   k_tiles  tiles of outputs on the loop of mma_tile.h, the reduction cut into
 //            slices where the tiles alone leave CUs idle; k_slices adds those up
-#include <algorithm>
 #include <type_traits>
 
 #include "dfp_internal.h"
