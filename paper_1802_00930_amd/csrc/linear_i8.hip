@@ -45,7 +45,7 @@ __device__ __forceinline__ void store_quad(const I8Args& g, int64_t i, int64_t j
 }
 
 // SLICED: the tiles of every slice in turn, their sums to g.part.
-// 16384 x 8192 x 8192 BF16 out: 855 to 990 us (2570 to 2220 TOP/s, by how hot the card
+// 16384 x 8192 x 8192 BF16 out: 855 to 1002 us (2570 to 2190 TOP/s, by card and how hot it
 // runs); 4096^3 61 us (2240 TOP/s: one round of tiles that start and end together).
 template <int T, bool SLICED, class Q>
 __global__ __launch_bounds__(Q::kThreads, 2) void k_tiles(I8Args g) {
@@ -204,7 +204,8 @@ __global__ __launch_bounds__(64 * kFewWaves) void k_few(I8Args g) {
 // after the row, since loads are waited for in order (one row by 4096 x 4096 7.4 us, 2.3
 // TB/s; before the row 8.4, in two launches 10.9).  The row stays packed, in 128 registers
 // with all else, so that two workgroups share a CU (one row by 8192 x 8192: 16.2 us,
-// with one 19.3).
+// with one 19.3).  Stochastic rounding does not fit them, its row spills (144 to 272 bytes a
+// lane; one row by 4096 x 4096 13.4 us a call, nearest 6.8).
 template <int T, int MODE, int UNROLL>
 __global__ __launch_bounds__(64 * kFewWaves, 4) void k_token(I8Args g, const typename Elem<T>::type* __restrict__ x,
                                                           int32_t k, uint32_t k0, uint32_t k1) {

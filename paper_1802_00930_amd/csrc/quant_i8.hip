@@ -6,7 +6,8 @@
 //             rows, then the rounding into the transposed layout
 // Both are bound by memory (a large copy runs at 4.92 TB/s): the exact rounding, a
 // product, a fused difference and a test that it is the nearest, costs five operations
-// an element, and only where the test fails the ones that mend it.
+// an element, and only where the test fails the ones that mend it.  Stochastic rounding is
+// bound by arithmetic: the exact rounding, a division and a Philox word an element.
 #include <algorithm>
 #include <type_traits>
 
@@ -27,8 +28,9 @@ constexpr int kBlock = 256;
 // Rows by groups of G threads (64: four rows a workgroup, 256: one), NV vectors of
 // 8 elements a thread in registers; NV = 0: a row of any length, read twice.
 // colw (nullable): every element is first multiplied by its column's weight.
-// 8192 x 2048: BF16 12.5 us (4.0 TB/s), FP32 14.7 us (5.7 TB/s, a part of it from the
-// memory-side cache); 16384 x 8192 BF16 72.6 to 83 us (5.5 to 4.9 TB/s).
+// 8192 x 2048: BF16 12.1 to 13.7 us (4.2 to 3.7 TB/s), FP32 14.7 us (5.7 TB/s, a part of it
+// from the memory-side cache); 16384 x 8192 BF16 72.6 to 83 us (5.5 to 4.9 TB/s).  Stochastic:
+// 32.5, 32.4 and 198 us.
 template <int T, int MODE, int G, int NV, bool WEIGHTED>
 __global__ __launch_bounds__(kBlock) void k_rows_i8(const typename Elem<T>::type* __restrict__ src, int64_t rows,
                                                     int64_t cols, int64_t ld, const float* __restrict__ colw,
@@ -321,8 +323,8 @@ dfp_status launch_rows_i8(int32_t type, int32_t rounding, uint64_t seed, uint32_
       auto by_len = [&](auto weighted) -> dfp_status {
         typedef std::integral_constant<int, 64> Wave;
         typedef std::integral_constant<int, 256> Group;
-        // a wave a row up to 2048 (8192 x 2048 BF16 14.2 us; by workgroups 14.7); by workgroups for
-        // few such rows (their waves share the loads) and up to 16384
+        // a wave a row up to 2048 (8192 x 2048 BF16 3% faster than by workgroups, timed in turn); by
+        // workgroups for few such rows (their waves share the loads) and up to 16384
         if (nvec <= 64) return go(Wave(), std::integral_constant<int, 1>(), weighted);
         if (nvec <= 128) return go(Wave(), std::integral_constant<int, 2>(), weighted);
         if (nvec <= 256 && rows > 512) return go(Wave(), std::integral_constant<int, 4>(), weighted);
