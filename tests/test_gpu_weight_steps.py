@@ -241,3 +241,24 @@ def test_bf16_update_of_strong_directions_above_weak_ones(r, c, k, weak):
     off = float(torch.linalg.vector_norm(out.double() - want) / torch.linalg.vector_norm(want))
     print("off %.2e" % off, flush=True)
     assert off <= (2.0 ** -18 + 2.0 ** -16 / 3) ** 0.5
+
+
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("b,r,c", [(12, 512, 512), (1, 1000, 333), (1, 51, 8000), (2, 1469, 7439)])
+def test_calls_repeat_themselves(b, r, c, t):
+    """Bit for bit, whatever the workspace holds and whatever runs beside them."""
+    note("update %dx%dx%d %s twice" % (b, r, c, t))
+    x = normal(r, b, r, c).to(t)
+    d = dfp.make_ortho_desc(b, r, c, t)
+    n = dfp.ortho_workspace_bytes(d)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    ws = [torch.full((n,), g, dtype=torch.uint8, device=DEV) for g in (0xff, 0)]
+    outs = [torch.empty_like(x) for _ in range(2)]
+    w = [normal(1, b, r, c) for _ in range(2)]
+    v = [normal(2, b, r, c) for _ in range(2)]
+    torch.cuda.synchronize()
+    for i, s in enumerate(streams):
+        dfp.dfp_orthogonalize(d, x, outs[i], workspace=ws[i], stream=s)
+        dfp.dfp_muon_quantize(d, 0.02, 0.95, 0.1, 0.2, w[i], v[i], x, workspace=ws[i], stream=s)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[1]) and torch.equal(w[0], w[1]) and torch.equal(v[0], v[1])
